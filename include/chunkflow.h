@@ -7,7 +7,8 @@
  * boundaries; Sec. 3.3 chunk-granular partial residency).
  *
  * Conventions
- *   - Every function returns 0 on success or a negative cf_status; cf_last_error() gives text.
+ *   - Every function returns 0 on success or a negative cf_status; cf_last_error() gives text.  A NULL context gives
+ *     that of the calling thread's last failed call without a context.
  *   - Pointers named `host_*` are host memory, everything inside cf_block_io is DEVICE memory.
  *   - The caller owns all host blobs and all device tensors it passes in.  The library owns its
  *     context, its events, the two staging slots, the per-block resident buffers and (when the
@@ -167,7 +168,7 @@ typedef struct {
  * cf_create validates the description and plans blob layout and chunking; it touches no GPU. */
 int cf_create(const cf_model_desc* desc, cf_ctx** out);
 int cf_destroy(cf_ctx* ctx);                                   /* syncs, frees everything it owns */
-const char* cf_last_error(const cf_ctx* ctx);                  /* ctx may be NULL: last create error */
+const char* cf_last_error(const cf_ctx* ctx);                  /* ctx may be NULL: see above */
 int cf_blob_bytes(const cf_ctx* ctx, uint64_t* out);            /* of block 0; every block's in a one-kind model */
 int cf_n_chunks(const cf_ctx* ctx, int32_t* out);
 /* tensors in blob order; *n is capacity on entry, count on return (call with out=NULL to query) */
@@ -305,6 +306,34 @@ int cf_op_checksum(const void* data, uint64_t bytes, uint64_t first_word, uint64
  * All calls on one GPU share that array: two calls whose kernels may overlap (different streams
  * without an ordering between them) race; calls on one stream, or ordered by events, are safe. */
 int cf_op_checksum_noalloc(const void* data, uint64_t bytes, uint64_t first_word, uint64_t* dev_out, void* stream);
+
+/* ---- rotary positions with several axes (time, height and width of a video token, say).
+ * Pair p = (2p, 2p + 1) of a head belongs to one axis and turns by pos[axis] * theta[axis]^(-j / n) radians, j its index among the
+ * n pairs of the axis; axes have the leading pairs one after the other, pairs that are left over are not turned.  Positions are
+ * integers of any size and sign: angles are exact to 1e-8 radians wherever they are (fixed point, see csrc/rope.h).
+ * cf_rope_plan is host arithmetic (some microseconds): make a plan once and keep it; it is a plain value and holds nothing. */
+#define CF_ROPE_AXES 4
+typedef enum { CF_BF16 = 0, CF_F32 = 1 } cf_dtype;
+typedef struct {
+    int32_t head_dim, n_axes, n_pairs, reserved;
+    uint64_t turn[64];           /* angle of pair p per position, in 2^-64 turns                  */
+    uint8_t axis[64];
+} cf_rope;
+/* axis_pairs[a] >= 1 pairs of axis a, head_dim / 2 (64 or 128) at most in all; theta[a] >= 1. */
+int cf_rope_plan(int32_t head_dim, int32_t n_axes, const int32_t* axis_pairs, const double* theta, cf_rope* out);
+/* cos and sin [n, head_dim/2] of pos [n, n_axes]: the tables that cf_block_io takes as rope_cos / rope_sin. */
+int cf_rope_tables(const cf_rope* rope, const int32_t* pos, int64_t n, float* cos_out, float* sin_out, void* stream);
+/* y = x turned, for one or two operands (q and k) of type `dtype` in one launch: [n, heads, head_dim], the last dimension dense, the
+ * others at any strides (elements, not negative, multiples of 16 bytes; pointers 16-byte aligned).  inverse: turned back, which is also the
+ * gradient of x from that of y.  In place: y = x with the same strides; outputs may otherwise overlap nothing.  Computed in fp32, rounded once. */
+typedef struct {
+    const void* x;
+    void* y;
+    int64_t x_row, x_head, y_row, y_head;
+    int32_t heads, reserved;
+} cf_rope_operand;
+int cf_rope_apply(const cf_rope* rope, const int32_t* pos, int64_t n, const cf_rope_operand* ops, int32_t n_ops, int32_t dtype,
+                  int32_t inverse, void* stream);
 
 #ifdef __cplusplus
 }

@@ -80,6 +80,20 @@ class cf_tune_choice(C.Structure):
     _fields_ = [("chunk_bytes", C.c_uint64), ("r", C.c_double), ("feasible", C.c_int32), ("sim", cf_sim_result)]
 
 
+CF_BF16, CF_F32 = 0, 1
+CF_ROPE_AXES = 4
+
+
+class cf_rope(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("n_axes", C.c_int32), ("n_pairs", C.c_int32), ("reserved", C.c_int32),
+                ("turn", C.c_uint64 * 64), ("axis", C.c_uint8 * 64)]
+
+
+class cf_rope_operand(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("y", C.c_void_p), ("x_row", C.c_int64), ("x_head", C.c_int64), ("y_row", C.c_int64), ("y_head", C.c_int64),
+                ("heads", C.c_int32), ("reserved", C.c_int32)]
+
+
 #: what include/chunkflow.h declares: the block path's contract
 CORE_EXPORTS = ["cf_create", "cf_destroy", "cf_last_error", "cf_blob_bytes", "cf_n_chunks", "cf_blob_layout",
                 "cf_set_block_kinds", "cf_block_kind_of", "cf_blob_bytes_of", "cf_n_chunks_of", "cf_blob_layout_of",
@@ -87,7 +101,8 @@ CORE_EXPORTS = ["cf_create", "cf_destroy", "cf_last_error", "cf_blob_bytes", "cf
                 "set_resident_fraction", "chunked_prefetch_begin", "chunked_prefetch_wait", "dit_block_fwd",
                 "cf_set_contention", "cf_comm_begin", "cf_comm_end", "cf_checksum_block", "cf_read_block", "cf_stats",
                 "cf_stats_reset", "cf_set_profiling", "cf_set_adaptive_waits", "cf_kernel_times", "cf_kernel_times_reset",
-                "cf_sync", "cf_op_checksum", "cf_op_checksum_noalloc"]
+                "cf_sync", "cf_op_checksum", "cf_op_checksum_noalloc",
+                "cf_rope_plan", "cf_rope_tables", "cf_rope_apply"]
 #: what include/chunkflow_diag.h declares: single-kernel hooks, planner views, the matrix-core rate probe
 DIAG_EXPORTS = ["cf_plan_attention", "cf_plan_block_attention", "cf_plan_linear", "cf_plan_block_linear", "cf_plan_block_meet", "cf_plan_block_fetch", "cf_op_linear", "cf_op_linear_residual", "cf_op_linear_residual_form",
                 "cf_op_attention", "cf_op_attention_form", "cf_op_ln_modulate", "cf_op_modvec", "cf_op_mfma_rate", "cf_op_mix_rate"]
@@ -160,6 +175,9 @@ def lib() -> C.CDLL:
         _lib.cf_op_modvec.argtypes = [C.c_void_p, C.c_uint64, C.c_uint64, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p]
         _lib.cf_op_mfma_rate.argtypes = [C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]
         _lib.cf_op_mix_rate.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]
+        _lib.cf_rope_plan.argtypes = [C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.POINTER(cf_rope)]
+        _lib.cf_rope_tables.argtypes = [C.POINTER(cf_rope), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]
+        _lib.cf_rope_apply.argtypes = [C.POINTER(cf_rope), C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p]
         _lib.cf_op_checksum.argtypes = [C.c_void_p, C.c_uint64, C.c_uint64, C.c_void_p, C.c_void_p]
         _lib.cf_op_checksum_noalloc.argtypes = [C.c_void_p, C.c_uint64, C.c_uint64, C.c_void_p, C.c_void_p]
     return _lib
@@ -475,3 +493,94 @@ def cf_op_checksum_noalloc(data, nbytes, first_word, dev_out, stream=None) -> No
     """Checksum of a device byte range into a device uint64 (torch int64 tensor of one element);
     enqueues only: the caller synchronises before reading dev_out."""
     _check(lib().cf_op_checksum_noalloc(_ptr(data), nbytes, first_word, _ptr(dev_out), _stream_handle(stream)))
+
+
+# ---- rotary positions.  The calls from here on look at their tensors' types, shapes, strides and devices, run on the device the tensors are on
+# and, without a stream, on torch's current one there.
+_TYPES: dict = {}
+
+
+def _refuse(cond, msg: str) -> None:
+    if cond:
+        raise ChunkflowError(CF_ERR_ARG, msg)
+
+
+def _dtype_of(t) -> int:
+    if not _TYPES:
+        import torch
+        _TYPES.update({torch.bfloat16: CF_BF16, torch.float32: CF_F32})
+    code = _TYPES.get(t.dtype)
+    _refuse(code is None, f"{t.dtype} is neither bfloat16 nor float32")
+    return code
+
+
+def _launch(fn, name: str, device, stream, *args) -> None:
+    """fn(*args, stream) on `device`, which has to be a GPU."""
+    import torch
+    _refuse(device.type != "cuda", f"{name}: tensors on {device}, not on a GPU")
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    _refuse(stream.device != device, f"{name}: a stream of {stream.device} for tensors on {device}")
+    if torch.cuda.current_device() == device.index:
+        _check(fn(*args, stream.cuda_stream))
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, stream.cuda_stream))
+
+
+def _dense(t, what: str, dtypes, shape, device=None) -> int:
+    """The pointer of a dense tensor of that shape and one of those types on `device`."""
+    _refuse(t.dtype not in dtypes, f"{what}: {t.dtype}, expected {' or '.join(str(d) for d in dtypes)}")
+    _refuse(tuple(t.shape) != tuple(shape), f"{what}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    _refuse(not t.is_contiguous(), f"{what} is not dense")
+    _refuse(device is not None and t.device != device, f"{what} is on {t.device}, other tensors on {device}")
+    return t.data_ptr()
+
+
+def cf_rope_plan(head_dim: int, axis_pairs, theta=10000.0) -> cf_rope:
+    """Plan of positions on len(axis_pairs) axes with that many pairs each; theta: one number or one per axis.  Host arithmetic: make it once."""
+    n = len(axis_pairs)
+    thetas = [float(v) for v in theta] if hasattr(theta, "__len__") else [float(theta)] * n
+    _refuse(len(thetas) != n, f"rope_plan: {len(thetas)} thetas for {n} axes")
+    out = cf_rope()
+    _check(lib().cf_rope_plan(head_dim, n, (C.c_int32 * max(1, n))(*[int(v) for v in axis_pairs]), (C.c_double * max(1, n))(*thetas), C.byref(out)))
+    return out
+
+
+def cf_rope_tables(rope: cf_rope, pos, cos_out, sin_out, stream=None) -> None:
+    """cos_out, sin_out [n, head_dim / 2] float32 of pos [n, axes] int32: what cf_block_io takes as rope_cos and rope_sin."""
+    import torch
+    n = pos.shape[0]
+    p = _dense(pos, "rope_tables: pos", (torch.int32,), (n, rope.n_axes))
+    c = _dense(cos_out, "rope_tables: cos_out", (torch.float32,), (n, rope.head_dim // 2), pos.device)
+    s = _dense(sin_out, "rope_tables: sin_out", (torch.float32,), (n, rope.head_dim // 2), pos.device)
+    _launch(lib().cf_rope_tables, "rope_tables", pos.device, stream, C.byref(rope), p, n, c, s)
+
+
+def _rope_operand(rope, x, y, n, like, which) -> tuple:
+    _refuse(x.dim() != 3 or x.shape[0] != n or x.shape[2] != rope.head_dim, f"rope_apply: {which} has shape {tuple(x.shape)}, expected ({n}, heads, {rope.head_dim})")
+    _refuse(y.shape != x.shape, f"rope_apply: {which} and its output differ in shape")
+    _refuse(x.dtype != like.dtype or y.dtype != like.dtype, f"rope_apply: {which}: one type for all operands")
+    xs, ys = x.stride(), y.stride()
+    _refuse(xs[2] != 1 or ys[2] != 1, f"rope_apply: {which}: the last dimension is not dense")
+    _refuse(x.device != like.device or y.device != like.device, f"rope_apply: {which}: operands on several devices")
+    heads = x.shape[1]
+    if n < 2:                   # the stride of a dimension of one says nothing
+        xs, ys = (0,) + xs[1:], (0,) + ys[1:]
+    if heads < 2:
+        xs, ys = (xs[0], 0), (ys[0], 0)
+    return x.data_ptr(), y.data_ptr(), xs[0], xs[1], ys[0], ys[1], heads, 0
+
+
+def cf_rope_apply(rope: cf_rope, pos, q, q_out, k=None, k_out=None, inverse: bool = False, stream=None) -> None:
+    """q_out = q [n, heads, head_dim] turned by pos [n, axes] int32 (inverse: turned back, the gradient), and k likewise if given; in place
+    where the output is the input."""
+    import torch
+    n = q.shape[0]
+    p = _dense(pos, "rope_apply: pos", (torch.int32,), (n, rope.n_axes), q.device)
+    _refuse((k is None) != (k_out is None), "rope_apply: k and k_out go together")
+    ops = (cf_rope_operand * 2)()
+    ops[0] = _rope_operand(rope, q, q_out, n, q, "q")
+    if k is not None:
+        ops[1] = _rope_operand(rope, k, k_out, n, q, "k")
+    _launch(lib().cf_rope_apply, "rope_apply", q.device, stream, C.byref(rope), p, n, ops, 1 if k is None else 2, _dtype_of(q), int(inverse))

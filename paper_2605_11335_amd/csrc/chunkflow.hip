@@ -9,7 +9,7 @@
 
 #include "context.h"
 
-static std::string g_create_err;
+static thread_local std::string g_create_err;     // of calls without a context, which any number of threads may make
 // The prefetch worker reports into a string of its own: the context's message belongs to the
 // caller's thread, which may be failing a call of its own at the same moment.
 static thread_local std::string* t_err_sink = nullptr;

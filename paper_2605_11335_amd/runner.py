@@ -135,6 +135,18 @@ class BlockRunner:
         io.workspace_bytes = ws.numel() - off
         return io
 
+    def rope_tables(self, rope: B.cf_rope, pos: torch.Tensor) -> Dict[str, torch.Tensor]:
+        """rope_cos and rope_sin of a block's rows at integer positions pos [n_local, axes], computed on the compute stream: to be
+        added to the tensors of make_io."""
+        if pos.shape[0] != self.cfg.n_local or rope.head_dim != self.cfg.head_dim:
+            raise B.ChunkflowError(B.CF_ERR_ARG, f"rope_tables: {self.cfg.n_local} rows of {self.cfg.head_dim}-wide heads expected")
+        t = {k: torch.empty(pos.shape[0], rope.head_dim // 2, dtype=torch.float32, device=self.device) for k in ("rope_cos", "rope_sin")}
+        self.compute.wait_stream(torch.cuda.current_stream(self.device))
+        B.cf_rope_tables(rope, pos, t["rope_cos"], t["rope_sin"], stream=self.compute)
+        for x in (pos, *t.values()):
+            x.record_stream(self.compute)
+        return t
+
     # ---- execution
     def begin(self, block: int) -> None:
         self.ctx.chunked_prefetch_begin(block, self.copy)
