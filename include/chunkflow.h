@@ -335,6 +335,67 @@ typedef struct {
 int cf_rope_apply(const cf_rope* rope, const int32_t* pos, int64_t n, const cf_rope_operand* ops, int32_t n_ops, int32_t dtype,
                   int32_t inverse, void* stream);
 
+/* ---- keys and values kept in 8 bits, in pages: of the frames a clip has so far, or of the text, whose keys and values are the same at
+ * every denoising step.  Everything is the caller's device memory, nothing is held by the library.
+ * A sequence's tokens lie in pages of page_tokens; row b of `table` names the pages of sequence b in order.  Sixteen consecutive tokens of a
+ * head are a group: e4m3 codes (finite to 448, NaN 0x7f, no infinity) that stand for code * 2^(byte - 127), one byte for K and one for V.
+ *   k      [n_pages][heads][page_tokens/16][head_dim/16][16 tokens][16 dims]
+ *   v      [n_pages][heads][page_tokens/16][head_dim][16 tokens]
+ *   scales [n_pages][heads][page_tokens/16][2]                                  (255: everything in the group is NaN)
+ * An entry of the table outside [0, n_pages) names no page: tokens there are not written, and no query sees them. */
+typedef struct {
+    uint8_t* k;
+    uint8_t* v;
+    uint8_t* scales;
+    const int32_t* table;        /* [n_seqs, table_width]                                          */
+    int32_t n_pages;
+    int32_t page_tokens;         /* a power of two from 16 to 4096                                 */
+    int32_t heads;
+    int32_t head_dim;            /* 64 or 128                                                      */
+    int32_t n_seqs;
+    int32_t table_width;
+} cf_kv_cache;
+/* Appends: rows [cu[b], cu[b+1]) of k and v become tokens lens[b], lens[b] + 1, ... of sequence b; k turned by pos on the way if a plan is
+ * given.  lens is what the sequences hold BEFORE the call and is not changed.  Rows outside [cu[0], cu[n_seqs]) are not read, tokens that
+ * the table has no room for are dropped.  The power of two of a group is the least that holds the largest value ( |a| + |b| of a pair that is
+ * turned) of its new tokens, and no less than that of the tokens it held; those are then requantised.  What is not finite is stored as NaN and takes
+ * no part in that.  A page that tokens are appended to belongs to one sequence only (full pages may be shared).  cu must not decrease. */
+typedef struct {
+    const void* k;               /* [n_tokens, heads, head_dim] of `dtype`, the last dimension dense; strides in elements,   */
+    const void* v;               /*   not negative, multiples of 16 bytes; pointers 16-byte aligned                          */
+    int64_t k_row, k_head, v_row, v_head;
+    const int32_t* cu;           /* [n_seqs + 1]                                                   */
+    const int32_t* lens;         /* [n_seqs]                                                       */
+    const cf_rope* rope;         /* host memory; NULL: k as it is                                  */
+    const int32_t* pos;          /* [n_tokens, rope->n_axes]                                       */
+    int32_t n_tokens;
+    int32_t dtype;               /* cf_dtype                                                       */
+} cf_kv_new;
+int cf_kv_append(const cf_kv_cache* cache, const cf_kv_new* tokens, void* stream);
+/* o = softmax(scale * q K^T) V for rows [cu[b], cu[b+1]) of q over the tokens [0, lens[b]) of sequence b (lens AFTER an append), query head i
+ * reading the cache's head i / (heads / cache heads).  causal: query j of n sees the tokens up to lens[b] - n + j.  A query that
+ * sees none gets zeros.  Rows of o outside [cu[0], cu[n_seqs]) stay as they are.  Tokens that a query does not see take no part,
+ * whatever their codes.  Accumulated in fp32; weights are rounded to bf16 for the second product.
+ * workspace: at least cf_kv_attention_workspace bytes, 256-byte aligned, nothing to initialise; calls that may overlap need one each.
+ * max_q: the most queries any sequence has; only plans the launch (0: n_tokens), and results do not depend on it being right beyond
+ * rounding.  With the same sizes and strides a call can be captured and replayed on changed tables, lengths and offsets. */
+typedef struct {
+    const uint16_t* q;           /* [n_tokens, heads, head_dim] bf16, as k above                   */
+    uint16_t* o;
+    int64_t q_row, q_head, o_row, o_head;
+    const int32_t* cu;
+    const int32_t* lens;
+    int32_t n_tokens;
+    int32_t heads;               /* a multiple of the cache's                                      */
+    int32_t max_q;
+    int32_t causal;
+    float scale;                 /* positive                                                       */
+    int32_t reserved;
+} cf_kv_query;
+int cf_kv_attention(const cf_kv_cache* cache, const cf_kv_query* queries, void* workspace, uint64_t workspace_bytes, void* stream);
+/* host arithmetic; looks at the cache's sizes and at n_tokens, heads and max_q */
+int cf_kv_attention_workspace(const cf_kv_cache* cache, const cf_kv_query* queries, uint64_t* bytes);
+
 #ifdef __cplusplus
 }
 #endif

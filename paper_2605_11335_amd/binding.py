@@ -94,6 +94,22 @@ class cf_rope_operand(C.Structure):
                 ("heads", C.c_int32), ("reserved", C.c_int32)]
 
 
+class cf_kv_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("scales", C.c_void_p), ("table", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("n_pages", "page_tokens", "heads", "head_dim", "n_seqs", "table_width")]
+
+
+class cf_kv_new(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)] + [(n, C.c_int64) for n in ("k_row", "k_head", "v_row", "v_head")] + \
+               [("cu", C.c_void_p), ("lens", C.c_void_p), ("rope", C.POINTER(cf_rope)), ("pos", C.c_void_p), ("n_tokens", C.c_int32), ("dtype", C.c_int32)]
+
+
+class cf_kv_query(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("o", C.c_void_p)] + [(n, C.c_int64) for n in ("q_row", "q_head", "o_row", "o_head")] + \
+               [("cu", C.c_void_p), ("lens", C.c_void_p)] + [(n, C.c_int32) for n in ("n_tokens", "heads", "max_q", "causal")] + \
+               [("scale", C.c_float), ("reserved", C.c_int32)]
+
+
 #: what include/chunkflow.h declares: the block path's contract
 CORE_EXPORTS = ["cf_create", "cf_destroy", "cf_last_error", "cf_blob_bytes", "cf_n_chunks", "cf_blob_layout",
                 "cf_set_block_kinds", "cf_block_kind_of", "cf_blob_bytes_of", "cf_n_chunks_of", "cf_blob_layout_of",
@@ -102,7 +118,7 @@ CORE_EXPORTS = ["cf_create", "cf_destroy", "cf_last_error", "cf_blob_bytes", "cf
                 "cf_set_contention", "cf_comm_begin", "cf_comm_end", "cf_checksum_block", "cf_read_block", "cf_stats",
                 "cf_stats_reset", "cf_set_profiling", "cf_set_adaptive_waits", "cf_kernel_times", "cf_kernel_times_reset",
                 "cf_sync", "cf_op_checksum", "cf_op_checksum_noalloc",
-                "cf_rope_plan", "cf_rope_tables", "cf_rope_apply"]
+                "cf_rope_plan", "cf_rope_tables", "cf_rope_apply", "cf_kv_append", "cf_kv_attention", "cf_kv_attention_workspace"]
 #: what include/chunkflow_diag.h declares: single-kernel hooks, planner views, the matrix-core rate probe
 DIAG_EXPORTS = ["cf_plan_attention", "cf_plan_block_attention", "cf_plan_linear", "cf_plan_block_linear", "cf_plan_block_meet", "cf_plan_block_fetch", "cf_op_linear", "cf_op_linear_residual", "cf_op_linear_residual_form",
                 "cf_op_attention", "cf_op_attention_form", "cf_op_ln_modulate", "cf_op_modvec", "cf_op_mfma_rate", "cf_op_mix_rate"]
@@ -178,6 +194,9 @@ def lib() -> C.CDLL:
         _lib.cf_rope_plan.argtypes = [C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.POINTER(cf_rope)]
         _lib.cf_rope_tables.argtypes = [C.POINTER(cf_rope), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]
         _lib.cf_rope_apply.argtypes = [C.POINTER(cf_rope), C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p]
+        _lib.cf_kv_append.argtypes = [C.POINTER(cf_kv_cache), C.POINTER(cf_kv_new), C.c_void_p]
+        _lib.cf_kv_attention.argtypes = [C.POINTER(cf_kv_cache), C.POINTER(cf_kv_query), C.c_void_p, C.c_uint64, C.c_void_p]
+        _lib.cf_kv_attention_workspace.argtypes = [C.POINTER(cf_kv_cache), C.POINTER(cf_kv_query), C.POINTER(C.c_uint64)]
         _lib.cf_op_checksum.argtypes = [C.c_void_p, C.c_uint64, C.c_uint64, C.c_void_p, C.c_void_p]
         _lib.cf_op_checksum_noalloc.argtypes = [C.c_void_p, C.c_uint64, C.c_uint64, C.c_void_p, C.c_void_p]
     return _lib
@@ -557,19 +576,19 @@ def cf_rope_tables(rope: cf_rope, pos, cos_out, sin_out, stream=None) -> None:
     _launch(lib().cf_rope_tables, "rope_tables", pos.device, stream, C.byref(rope), p, n, c, s)
 
 
+def _strides(t) -> tuple:
+    """Strides of rows and heads of a [n, heads, head_dim] tensor; that of a dimension of one says nothing and becomes 0."""
+    s, n = t.stride(), t.shape
+    return s[0] if n[0] > 1 else 0, s[1] if n[1] > 1 else 0
+
+
 def _rope_operand(rope, x, y, n, like, which) -> tuple:
     _refuse(x.dim() != 3 or x.shape[0] != n or x.shape[2] != rope.head_dim, f"rope_apply: {which} has shape {tuple(x.shape)}, expected ({n}, heads, {rope.head_dim})")
     _refuse(y.shape != x.shape, f"rope_apply: {which} and its output differ in shape")
     _refuse(x.dtype != like.dtype or y.dtype != like.dtype, f"rope_apply: {which}: one type for all operands")
-    xs, ys = x.stride(), y.stride()
-    _refuse(xs[2] != 1 or ys[2] != 1, f"rope_apply: {which}: the last dimension is not dense")
+    _refuse(x.stride(2) != 1 or y.stride(2) != 1, f"rope_apply: {which}: the last dimension is not dense")
     _refuse(x.device != like.device or y.device != like.device, f"rope_apply: {which}: operands on several devices")
-    heads = x.shape[1]
-    if n < 2:                   # the stride of a dimension of one says nothing
-        xs, ys = (0,) + xs[1:], (0,) + ys[1:]
-    if heads < 2:
-        xs, ys = (xs[0], 0), (ys[0], 0)
-    return x.data_ptr(), y.data_ptr(), xs[0], xs[1], ys[0], ys[1], heads, 0
+    return x.data_ptr(), y.data_ptr(), *_strides(x), *_strides(y), x.shape[1], 0
 
 
 def cf_rope_apply(rope: cf_rope, pos, q, q_out, k=None, k_out=None, inverse: bool = False, stream=None) -> None:
@@ -584,3 +603,72 @@ def cf_rope_apply(rope: cf_rope, pos, q, q_out, k=None, k_out=None, inverse: boo
     if k is not None:
         ops[1] = _rope_operand(rope, k, k_out, n, q, "k")
     _launch(lib().cf_rope_apply, "rope_apply", q.device, stream, C.byref(rope), p, n, ops, 1 if k is None else 2, _dtype_of(q), int(inverse))
+
+
+# ---- keys and values kept in 8 bits
+class KVCache:
+    """Handle of a paged cache for cf_kv_append and cf_kv_attention (make_kv_cache); keeps its tensors alive."""
+
+    def __init__(self, k, v, scales, table):
+        import torch
+        _refuse(k.dim() != 6 or tuple(k.shape[4:]) != (16, 16), f"kv_cache: k has shape {tuple(k.shape)}, expected [pages, heads, page / 16, head_dim / 16, 16, 16]")
+        pages, heads, groups, chunks = k.shape[:4]
+        codes = (torch.uint8, torch.float8_e4m3fn)
+        _refuse(table.dim() != 2, f"kv_cache: table has shape {tuple(table.shape)}, expected [sequences, pages per sequence]")
+        self.device, self.head_dim, self.heads, self.n_seqs = k.device, chunks * 16, heads, table.shape[0]
+        self.tensors = (k, v, scales, table)
+        self.c = cf_kv_cache(_dense(k, "kv_cache: k", codes, k.shape), _dense(v, "kv_cache: v", codes, (pages, heads, groups, chunks * 16, 16), k.device),
+                             _dense(scales, "kv_cache: scales", (torch.uint8,), (pages, heads, groups, 2), k.device),
+                             _dense(table, "kv_cache: table", (torch.int32,), table.shape, k.device),
+                             pages, groups * 16, heads, chunks * 16, table.shape[0], table.shape[1])
+        self.ref = C.byref(self.c)
+
+
+def make_kv_cache(k, v, scales, table) -> KVCache:
+    """Cache over the caller's tensors, dense: k [pages, heads, page / 16, head_dim / 16, 16, 16] and v [pages, heads, page / 16, head_dim, 16] uint8 (or
+    float8_e4m3fn), scales [pages, heads, page / 16, 2] uint8, table [sequences, pages per sequence] int32."""
+    return KVCache(k, v, scales, table)
+
+
+def _batch(cache, what: str, cu, lens) -> tuple:
+    import torch
+    return _dense(cu, what + ": cu", (torch.int32,), (cache.n_seqs + 1,), cache.device), _dense(lens, what + ": lens", (torch.int32,), (cache.n_seqs,), cache.device)
+
+
+def cf_kv_append(cache: KVCache, k, v, cu, lens, rope: Optional[cf_rope] = None, pos=None, stream=None) -> None:
+    """Rows cu[b] .. cu[b+1] of k and v [tokens, heads, head_dim] (bf16 or fp32) become tokens lens[b], ... of sequence b, k turned by pos if a plan is given."""
+    import torch
+    n, want = k.shape[0], (cache.heads, cache.head_dim)
+    _refuse(k.dim() != 3 or k.shape[1:] != want or v.shape != k.shape, f"kv_append: k {tuple(k.shape)} and v {tuple(v.shape)}, expected [tokens, {want[0]}, {want[1]}]")
+    _refuse(v.dtype != k.dtype, "kv_append: k and v differ in type")
+    _refuse(k.stride(2) != 1 or v.stride(2) != 1, "kv_append: the last dimension is not dense")
+    _refuse(k.device != cache.device or v.device != cache.device, "kv_append: tensors on several devices")
+    _refuse((rope is None) != (pos is None), "kv_append: a plan and positions go together")
+    at = None if rope is None else _dense(pos, "kv_append: pos", (torch.int32,), (n, rope.n_axes), cache.device)
+    x = cf_kv_new(k.data_ptr(), v.data_ptr(), *_strides(k), *_strides(v), *_batch(cache, "kv_append", cu, lens),
+                  None if rope is None else C.pointer(rope), at, n, _dtype_of(k))
+    _launch(lib().cf_kv_append, "kv_append", cache.device, stream, cache.ref, C.byref(x))
+
+
+def cf_kv_attention_workspace(cache: KVCache, q, max_q: int = 0) -> int:
+    """Bytes of workspace that cf_kv_attention needs for queries of q's shape [tokens, heads, head_dim]."""
+    out = C.c_uint64()
+    x = cf_kv_query(n_tokens=q.shape[0], heads=q.shape[1], max_q=max_q)
+    _check(lib().cf_kv_attention_workspace(cache.ref, C.byref(x), C.byref(out)))
+    return out.value
+
+
+def cf_kv_attention(cache: KVCache, q, o, cu, lens, causal: bool = False, scale: Optional[float] = None, max_q: int = 0, workspace=None, stream=None) -> None:
+    """o = softmax(scale q K^T) V for rows cu[b] .. cu[b+1] of q [tokens, heads, head_dim] (bf16) over the first lens[b] tokens of sequence b; scale: 1 / sqrt(head_dim)
+    if not given.  workspace: a dense tensor of cf_kv_attention_workspace bytes."""
+    import torch
+    n = q.shape[0]
+    _refuse(q.dim() != 3 or q.shape[2] != cache.head_dim or o.shape != q.shape, f"kv_attention: q {tuple(q.shape)} and o {tuple(o.shape)}, expected [tokens, heads, {cache.head_dim}]")
+    _refuse(q.dtype != torch.bfloat16 or o.dtype != torch.bfloat16, "kv_attention: q and o must be bfloat16")
+    _refuse(q.stride(2) != 1 or o.stride(2) != 1, "kv_attention: the last dimension is not dense")
+    _refuse(q.device != cache.device or o.device != cache.device or (workspace is not None and workspace.device != cache.device), "kv_attention: tensors on several devices")
+    _refuse(workspace is not None and not workspace.is_contiguous(), "kv_attention: the workspace is not dense")
+    x = cf_kv_query(q.data_ptr(), o.data_ptr(), *_strides(q), *_strides(o), *_batch(cache, "kv_attention", cu, lens), n, q.shape[1], max_q, int(causal),
+                    cache.head_dim ** -0.5 if scale is None else scale, 0)
+    _launch(lib().cf_kv_attention, "kv_attention", cache.device, stream, cache.ref, C.byref(x), _ptr(workspace),
+            0 if workspace is None else workspace.numel() * workspace.element_size())

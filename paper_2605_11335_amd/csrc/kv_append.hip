@@ -1,0 +1,240 @@
+// New tokens into a paged 8-bit cache: keys turned by their positions on the way, keys and values as e4m3 codes with one power of two per
+// group of 16 tokens (kv_cache.h).  Bound by HBM: 2 or 4 bytes per element in, 1 out.
+//
+// A power of two costs e4m3 no precision (its own exponent takes up what a finer factor would), and codes move to a larger one exactly unless they
+// become subnormal; so a group that is filled token by token keeps the codes it has, moved where a later token needs a larger power.
+// The power is taken from what goes in, not from what comes out of the rotation: |a| + |b| bounds a pair under any angle and is the
+// same number in any arithmetic, so that neither positions nor the last bit of a sine decide over it.
+#include "context.h"
+#include "kv_cache.h"
+#include "rope.h"
+
+namespace {
+
+constexpr int E_LEAST = -100;          // a group's least power: |x| below 2^-110 becomes zero
+
+struct AppendArgs {
+    KvView c;
+    cf_rope r;
+    const void *k, *v;
+    int64_t k_row, k_head, v_row, v_head;
+    const int32_t *cu, *lens, *pos;
+    int32_t n_tokens;
+};
+
+// The least e with m <= 224 * 2^e; m is half of what has to fit under 448 * 2^e (|a| + |b| itself could pass the fp32 range).
+__device__ __forceinline__ int power_for(float m) {
+    if (!(m > 0.0f)) return E_LEAST;
+    const int e = __builtin_amdgcn_frexp_expf(m) - 8 + (__builtin_amdgcn_frexp_mantf(m) > 0.875f);
+    return max(e, E_LEAST);
+}
+
+// x * 2^-e for two values as codes in the low 16 bits; what is not finite becomes the NaN code.
+__device__ __forceinline__ float to_range(float x, int e) {
+    const float y = __builtin_ldexpf(x, -e);
+    return fabsf(x) < INFINITY ? __builtin_amdgcn_fmed3f(y, -448.0f, 448.0f) : __uint_as_float(0x7fc00000u);
+}
+__device__ __forceinline__ uint32_t codes2(float a, float b, int e) {
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(to_range(a, e), to_range(b, e), 0, false) & 0xffffu;
+}
+// four codes at a power larger by `up`
+__device__ __forceinline__ uint32_t moved(uint32_t w, int up) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    const f2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+    int r = __builtin_amdgcn_cvt_pk_fp8_f32(__builtin_ldexpf(a[0], -up), __builtin_ldexpf(a[1], -up), 0, false);
+    r = __builtin_amdgcn_cvt_pk_fp8_f32(__builtin_ldexpf(b[0], -up), __builtin_ldexpf(b[1], -up), r, true);
+    return (uint32_t)r;
+}
+// LDS accesses of this wave before and after it keep their order
+__device__ __forceinline__ void lds_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+__device__ __forceinline__ float wave_max(float m) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    return m;
+}
+
+template <class T>
+__device__ __forceinline__ void load_pair(const T* p, float& a, float& b) {
+    if constexpr (sizeof(T) == 2) {
+        const uint32_t w = *(const uint32_t*)p;
+        a = __uint_as_float(w << 16);
+        b = __uint_as_float(w & 0xffff0000u);
+    } else {
+        const float2 w = *(const float2*)p;
+        a = w.x;
+        b = w.y;
+    }
+}
+
+// A wave has one group at a time, all of it: lane = a pair of dims, for 16 tokens (8 with 64-wide heads, whose other half of the lanes has the other 8).
+// Groups of a launch: sequence b, whose tokens are rows [cu[b], cu[b+1]), touches at most (n - 1) / 16 + 2 of them and owns the items from
+// S(b) = cu[b] / 16 + 2 b on, so that an item finds its sequence by a search of S and no order among items is needed.
+template <class T, int HD, bool ROPE>
+__global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
+    constexpr int PAIRS = HD / 2, TPL = PAIRS / 4, STEP = 16 * 16 + 16;       // tokens per lane; a chunk's place in LDS
+    __shared__ __attribute__((aligned(16))) uint8_t stage[4][HD / 16 * STEP];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int item = blockIdx.x, B = a.c.n_seqs;
+    int b = -1;
+    for (int base = 0; base < B; base += 64) {
+        const int i = base + lane;
+        const bool before = i < B && (kv_clamped(a.cu[i], 0, a.n_tokens) >> 4) + 2 * i <= item;
+        b += __popcll(__ballot(before));
+    }
+    if (b < 0) return;
+    const int start = kv_clamped(a.cu[b], 0, a.n_tokens), n = kv_clamped(a.cu[b + 1], start, a.n_tokens) - start;
+    const int len = kv_clamped(a.lens[b], 0, a.c.capacity);
+    const int nth = item - ((start >> 4) + 2 * b);
+    const int64_t first = ((int64_t)(len >> 4) + nth) << 4;
+    if (nth < 0 || first >= (int64_t)len + n || first >= a.c.capacity) return;
+    const int p0 = (int)first, lo = max(len - p0, 0), hi = (int)min((int64_t)16, min((int64_t)len + n, (int64_t)a.c.capacity) - p0);      // new slots
+    if (lo >= hi || kv_group(a.c, b, 0, p0) < 0) return;
+    const int pair = lane % PAIRS, s0 = lane / PAIRS * TPL;
+    const int64_t row0 = start + (p0 - len);                                   // of slot 0; slots in [lo, hi) have a row
+
+    float cs[TPL], sn[TPL];
+    if constexpr (ROPE) {
+        const uint64_t turn = a.r.turn[pair];
+        const int axis = a.r.axis[pair];
+#pragma unroll
+        for (int t = 0; t < TPL; ++t) {
+            const int slot = kv_clamped(s0 + t, lo, hi - 1);
+            rope_sincos(turn, a.pos[(row0 + slot) * a.r.n_axes + axis], cs[t], sn[t]);
+        }
+    }
+    for (int h = blockIdx.y * 4 + wave; h < a.c.heads; h += 4 * gridDim.y) {
+        const int g = kv_group(a.c, b, h, p0);
+        float ka[TPL], kb[TPL], va[TPL], vb[TPL];
+        float mk = 0.0f, mv = 0.0f;
+#pragma unroll
+        for (int t = 0; t < TPL; ++t) {
+            const int64_t row = row0 + kv_clamped(s0 + t, lo, hi - 1);         // slots without a new token repeat one that has
+            load_pair((const T*)a.k + row * a.k_row + h * a.k_head + 2 * pair, ka[t], kb[t]);
+            load_pair((const T*)a.v + row * a.v_row + h * a.v_head + 2 * pair, va[t], vb[t]);
+        }
+#pragma unroll
+        for (int t = 0; t < TPL; ++t) {
+            auto finite = [](float x) { x = fabsf(x); return x < INFINITY ? 0.5f * x : 0.0f; };
+            if constexpr (ROPE) {
+                const float m = 0.5f * fabsf(ka[t]) + 0.5f * fabsf(kb[t]);
+                mk = fmaxf(mk, m < INFINITY ? m : 0.0f);
+                rope_turn(ka[t], kb[t], cs[t], sn[t]);
+            } else {
+                mk = fmaxf(mk, fmaxf(finite(ka[t]), finite(kb[t])));
+            }
+            mv = fmaxf(mv, fmaxf(finite(va[t]), finite(vb[t])));
+        }
+        int ek = power_for(wave_max(mk)), ev = power_for(wave_max(mv)), up_k = 0, up_v = 0;
+        uint16_t* const scale = (uint16_t*)(a.c.scales + 2 * (int64_t)g);
+        if (lo > 0) {                                                          // tokens that were there: their power at least
+            const uint32_t was = *scale;
+            const int was_k = (int)(was & 255u) - 127, was_v = (int)(was >> 8) - 127;
+            ek = max(ek, was_k);
+            ev = max(ev, was_v);
+            up_k = ek - was_k;
+            up_v = ev - was_v;
+        }
+        uint8_t* const kg = a.c.k + (int64_t)g * (16 * HD);
+        uint8_t* const vg = a.c.v + (int64_t)g * (16 * HD);
+        // K: through LDS, from two dims of many tokens to 16 dims of one
+        uint8_t* const my = stage[wave];
+#pragma unroll
+        for (int t = 0; t < TPL; ++t)
+            *(uint16_t*)(my + (pair >> 3) * STEP + (s0 + t) * 16 + (pair & 7) * 2) = (uint16_t)codes2(ka[t], kb[t], ek);
+        lds_order();
+#pragma unroll
+        for (int i = 0; i < HD / 64; ++i) {
+            const int at = i * 64 + lane, chunk = at >> 4, slot = at & 15;
+            uint32x4 w = *(const uint32x4*)(my + chunk * STEP + slot * 16);
+            if (slot >= lo && slot < hi) {
+                *(uint32x4*)(kg + at * 16) = w;
+            } else if (slot < lo && up_k > 0) {
+                w = *(const uint32x4*)(kg + at * 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = moved(w[e], up_k);
+                *(uint32x4*)(kg + at * 16) = w;
+            }
+        }
+        lds_order();                                                           // the next head's codes go to the same place
+        // V: a lane's two dims of its tokens as they lie in memory; what a partly filled group holds besides stays
+#pragma unroll
+        for (int d = 0; d < 2; ++d) {
+            uint32_t* const p = (uint32_t*)(vg + (2 * pair + d) * 16 + s0);
+            uint32_t w[TPL / 4], old[TPL / 4];
+#pragma unroll
+            for (int i = 0; i < TPL / 4; ++i) {
+                const float* const x = d ? vb : va;
+                w[i] = codes2(x[4 * i], x[4 * i + 1], ev) | codes2(x[4 * i + 2], x[4 * i + 3], ev) << 16;
+                old[i] = 0;
+            }
+            if (lo > 0 || hi < 16) {
+#pragma unroll
+                for (int i = 0; i < TPL / 4; ++i) {
+                    old[i] = p[i];
+                    const uint32_t low = moved(old[i], up_v);
+                    uint32_t r = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int slot = s0 + 4 * i + e;
+                        const uint32_t mask = 255u << (8 * e);
+                        r |= (slot >= hi ? old[i] : slot >= lo ? w[i] : up_v > 0 ? low : old[i]) & mask;
+                    }
+                    w[i] = r;
+                }
+            }
+            if constexpr (TPL == 16) *(uint32x4*)p = uint32x4{w[0], w[1], w[2], w[3]};
+            else *(uint32x2*)p = uint32x2{w[0], w[1]};
+        }
+        if (lane == 0) *scale = (uint16_t)((ek + 127) | (ev + 127) << 8);
+    }
+}
+
+template <class T, int HD>
+void launch(const AppendArgs& a, bool rope, dim3 grid, hipStream_t s) {
+    if (rope) hipLaunchKernelGGL((kv_append_kernel<T, HD, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((kv_append_kernel<T, HD, false>), grid, dim3(256), 0, s, a);
+}
+
+}  // namespace
+
+extern "C" int cf_kv_append(const cf_kv_cache* cache, const cf_kv_new* x, void* stream) {
+    if (const char* bad = kv_bad(cache)) return cf_fail(nullptr, CF_ERR_ARG, "kv_append: %s", bad);
+    if (!x) return cf_fail(nullptr, CF_ERR_ARG, "kv_append: null tokens");
+    if (x->dtype != CF_BF16 && x->dtype != CF_F32) return cf_fail(nullptr, CF_ERR_ARG, "kv_append: type %d is neither CF_BF16 nor CF_F32", x->dtype);
+    if (x->n_tokens < 0) return cf_fail(nullptr, CF_ERR_ARG, "kv_append: %d tokens", x->n_tokens);
+    if (x->n_tokens == 0 || cache->n_seqs == 0) return CF_OK;
+    if (!x->k || !x->v || !x->cu || !x->lens) return cf_fail(nullptr, CF_ERR_ARG, "kv_append: null operand");
+    if (((uintptr_t)x->k | (uintptr_t)x->v) % 16 || ((uintptr_t)x->cu | (uintptr_t)x->lens | (uintptr_t)x->pos) % 4)
+        return cf_fail(nullptr, CF_ERR_ARG, "kv_append: k and v must be 16-byte aligned, offsets, lengths and positions 4");
+    const int es = x->dtype == CF_BF16 ? 2 : 4;
+    for (const int64_t st : {x->k_row, x->k_head, x->v_row, x->v_head})
+        if (st < 0 || st > (int64_t)1 << 40 || st * es % 16) return cf_fail(nullptr, CF_ERR_ARG, "kv_append: strides must be multiples of 16 bytes and not negative");
+    if (x->rope) {
+        if (const char* bad = rope_bad(x->rope)) return cf_fail(nullptr, CF_ERR_ARG, "kv_append: rotation: %s", bad);
+        if (x->rope->head_dim != cache->head_dim) return cf_fail(nullptr, CF_ERR_ARG, "kv_append: the plan turns %d-wide heads, the cache has %d", x->rope->head_dim, cache->head_dim);
+        if (!x->pos) return cf_fail(nullptr, CF_ERR_ARG, "kv_append: a rotation without positions");
+    }
+    const int64_t items = x->n_tokens / 16 + 2ll * cache->n_seqs;
+    if (items > 0x7fffffff) return cf_fail(nullptr, CF_ERR_ARG, "kv_append: too many tokens and sequences");
+    AppendArgs a = {};
+    a.c = kv_view(*cache);
+    if (x->rope) a.r = *x->rope;
+    a.k = x->k; a.v = x->v;
+    a.k_row = x->k_row; a.k_head = x->k_head; a.v_row = x->v_row; a.v_head = x->v_head;
+    a.cu = x->cu; a.lens = x->lens; a.pos = x->pos;
+    a.n_tokens = x->n_tokens;
+    const dim3 grid((unsigned)items, (unsigned)((cache->heads + 3) / 4));
+    hipStream_t s = (hipStream_t)stream;
+    if (x->dtype == CF_BF16) {
+        if (cache->head_dim == 128) launch<bf16, 128>(a, x->rope != nullptr, grid, s);
+        else launch<bf16, 64>(a, x->rope != nullptr, grid, s);
+    } else {
+        if (cache->head_dim == 128) launch<float, 128>(a, x->rope != nullptr, grid, s);
+        else launch<float, 64>(a, x->rope != nullptr, grid, s);
+    }
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? CF_OK : cf_fail(nullptr, CF_ERR_HIP, "kv_append launch: %s", hipGetErrorString(e));
+}

@@ -1,0 +1,104 @@
+"""Calls on a paged 8-bit cache that are refused before a GPU is touched."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_11335_amd import binding as B
+from tests.kvutil import E4M3, power
+
+HERE = 1 << 20          # a made-up aligned address: these calls are refused before anything is read
+
+
+def cache(**kw):
+    f = dict(k=HERE, v=HERE * 2, scales=HERE * 3, table=HERE * 4, n_pages=10, page_tokens=64, heads=4, head_dim=128, n_seqs=3, table_width=5)
+    f.update(kw)
+    return B.cf_kv_cache(**f)
+
+
+def new(**kw):
+    f = dict(k=HERE * 5, v=HERE * 6, k_row=512, k_head=128, v_row=512, v_head=128, cu=HERE * 7, lens=HERE * 8, n_tokens=9, dtype=B.CF_BF16)
+    f.update(kw)
+    return B.cf_kv_new(**f)
+
+
+def query(**kw):
+    f = dict(q=HERE * 5, o=HERE * 6, q_row=1024, q_head=128, o_row=1024, o_head=128, cu=HERE * 7, lens=HERE * 8, n_tokens=9, heads=8, max_q=0, causal=0, scale=0.1)
+    f.update(kw)
+    return B.cf_kv_query(**f)
+
+
+BAD_CACHES = [dict(k=None), dict(v=None), dict(scales=None), dict(table=None), dict(k=HERE + 8), dict(v=HERE + 1), dict(scales=HERE + 1), dict(table=HERE + 2),
+              dict(n_pages=0), dict(page_tokens=8), dict(page_tokens=48), dict(page_tokens=8192), dict(heads=0), dict(head_dim=96), dict(n_seqs=-1),
+              dict(table_width=0), dict(n_pages=2 ** 30), dict(table_width=2 ** 26)]
+
+
+@pytest.mark.parametrize("bad", BAD_CACHES)
+def test_caches_that_are_refused(bad):
+    c, n = cache(**bad), C.c_uint64()
+    for rc, name in ((B.lib().cf_kv_append(C.byref(c), C.byref(new()), None), b"kv_append"), (B.lib().cf_kv_attention(C.byref(c), C.byref(query()), None, 0, None), b"kv_attention"),
+                     (B.lib().cf_kv_attention_workspace(C.byref(c), C.byref(query()), C.byref(n)), b"kv_attention_workspace")):
+        assert rc == B.CF_ERR_ARG
+    assert name in B.lib().cf_last_error(None)
+
+
+@pytest.mark.parametrize("bad", [dict(k=None), dict(v=None), dict(cu=None), dict(lens=None), dict(k=HERE + 8), dict(v=HERE + 2), dict(cu=HERE + 2), dict(lens=HERE + 1), dict(n_tokens=-1),
+                                 dict(dtype=2), dict(dtype=-1), dict(k_row=511), dict(v_head=-128), dict(k_head=4)])
+def test_appends_that_are_refused(bad):
+    assert B.lib().cf_kv_append(C.byref(cache()), C.byref(new(**bad)), None) == B.CF_ERR_ARG
+    assert b"kv_append" in B.lib().cf_last_error(None)
+
+
+def test_rotations_that_do_not_fit_the_cache():
+    right, wrong = B.cf_rope_plan(128, [64]), B.cf_rope_plan(64, [32])
+    for rope, pos in ((wrong, HERE * 9), (right, None), (right, HERE * 9 + 2), (B.cf_rope(), HERE * 9)):
+        assert B.lib().cf_kv_append(C.byref(cache()), C.byref(new(rope=C.pointer(rope), pos=pos)), None) == B.CF_ERR_ARG
+
+
+@pytest.mark.parametrize("bad", [dict(q=None), dict(o=None), dict(cu=None), dict(lens=None), dict(q=HERE + 8), dict(o=HERE + 2), dict(cu=HERE + 3), dict(n_tokens=-1), dict(max_q=-1),
+                                 dict(heads=6), dict(heads=0), dict(heads=1 << 20), dict(q_row=1020), dict(o_head=-128), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.inf),
+                                 dict(scale=math.nan)])
+def test_queries_that_are_refused(bad):
+    ws = C.c_uint64()
+    rc = B.lib().cf_kv_attention_workspace(C.byref(cache()), C.byref(query()), C.byref(ws))
+    assert rc == B.CF_OK
+    assert B.lib().cf_kv_attention(C.byref(cache()), C.byref(query(**bad)), HERE * 16, ws.value, None) == B.CF_ERR_ARG
+    assert b"kv_attention" in B.lib().cf_last_error(None)
+
+
+def test_nothing_to_do_is_no_error():
+    assert B.lib().cf_kv_append(C.byref(cache()), C.byref(new(n_tokens=0)), None) == B.CF_OK
+    assert B.lib().cf_kv_append(C.byref(cache(n_seqs=0)), C.byref(new()), None) == B.CF_OK
+    assert B.lib().cf_kv_attention(C.byref(cache()), C.byref(query(n_tokens=0)), None, 0, None) == B.CF_OK
+    assert B.lib().cf_kv_attention(C.byref(cache(n_seqs=0)), C.byref(query()), None, 0, None) == B.CF_OK
+
+
+def test_the_binding_refuses_tensors_that_do_not_fit():
+    u8 = lambda *s: torch.zeros(*s, dtype=torch.uint8)          # noqa: E731
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)         # noqa: E731
+    k, v, s, t = u8(7, 2, 4, 4, 16, 16), u8(7, 2, 4, 64, 16), u8(7, 2, 4, 2), i32(3, 2)
+    c = B.make_kv_cache(k, v, s, t)
+    assert (c.c.n_pages, c.c.page_tokens, c.c.heads, c.c.head_dim, c.c.n_seqs, c.c.table_width) == (7, 64, 2, 64, 3, 2)
+    B.make_kv_cache(k.view(torch.float8_e4m3fn), v.view(torch.float8_e4m3fn), s, t)
+    x, q, cu, lens = torch.zeros(5, 2, 64), torch.zeros(5, 4, 64, dtype=torch.bfloat16), i32(4), i32(3)
+    plan, ws = B.cf_rope_plan(64, [16, 16]), u8(1 << 20)
+    for bad in (lambda: B.make_kv_cache(k[..., :8], v, s, t), lambda: B.make_kv_cache(k, v[:6], s, t), lambda: B.make_kv_cache(k, v, s.int(), t), lambda: B.make_kv_cache(k, v, s, t.long()),
+                lambda: B.make_kv_cache(k, v, s, t[0]), lambda: B.make_kv_cache(k.transpose(0, 1), v, s, t), lambda: B.make_kv_cache(k.float(), v, s, t),
+                lambda: B.cf_kv_append(c, x[:, :1], x[:, :1], cu, lens), lambda: B.cf_kv_append(c, x, x.bfloat16(), cu, lens), lambda: B.cf_kv_append(c, x.double(), x.double(), cu, lens),
+                lambda: B.cf_kv_append(c, x, x, cu[:3], lens), lambda: B.cf_kv_append(c, x, x, cu.long(), lens), lambda: B.cf_kv_append(c, x, x, cu, i32(4)),
+                lambda: B.cf_kv_append(c, x, x, cu, lens, plan, i32(5, 1)), lambda: B.cf_kv_append(c, x, x, cu, lens, plan, None), lambda: B.cf_kv_append(c, x.transpose(1, 2), x, cu, lens),
+                lambda: B.cf_kv_append(c, x, x, cu, lens),                                                             # in order, but not on a GPU
+                lambda: B.cf_kv_attention(c, q.float(), q.float(), cu, lens), lambda: B.cf_kv_attention(c, q, q[:4], cu, lens), lambda: B.cf_kv_attention(c, q[:, :, :32], q[:, :, :32], cu, lens),
+                lambda: B.cf_kv_attention(c, q, q, cu[1:], lens), lambda: B.cf_kv_attention(c, q, q, cu, lens, workspace=ws[::2]), lambda: B.cf_kv_attention(c, q, q, cu, lens, workspace=ws)):
+        with pytest.raises(B.ChunkflowError) as e:
+            bad()
+        assert e.value.code == B.CF_ERR_ARG
+
+
+def test_the_helpers_know_the_format():
+    """The tests' own e4m3 table and power rule, against torch's type and by hand."""
+    every = torch.arange(256, dtype=torch.uint8)
+    assert np.array_equal(every.view(torch.float8_e4m3fn).double().numpy(), E4M3, equal_nan=True)
+    assert [power(x) for x in (0.0, 448.0, 449.0, 224.0, 1.0, 1e-40)] == [-100, 0, 1, -1, -8, -100]
