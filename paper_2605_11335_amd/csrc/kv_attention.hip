@@ -1,83 +1,357 @@
 // Softmax attention of ragged queries over a paged 8-bit cache (kv_cache.h).  Each group's codes are multiplied by its power of two; keys past a
 // sequence's length, of pages that the table does not name and, causal, behind the query take no part, whatever their codes are.
-//
-// A wave has one query of one head and goes through the keys 64 at a time, a lane to each: scores, running maximum and sum of the softmax, then a
-// lane per output dim over the 64 weights.
+#include <algorithm>
 #include <cmath>
 
 #include "context.h"
-#include "kv_cache.h"
+#include "kv_tile.h"
 
 namespace {
 
-struct AttendArgs {
-    KvView c;
-    const bf16* q;
-    bf16* o;
-    int64_t q_row, q_head, o_row, o_head;
-    const int32_t *cu, *lens;
-    int32_t n_tokens, heads, times;        // times: query heads per key head
-    int32_t causal;
-    float c2;                              // scale * log2(e)
-};
+// ---------------------------------------------------------------------------------------------
+// Few columns: at most 32 for a (sequence, key head), single tokens above all.  Bound by reading the cache once.  Operand fragments come straight from
+// memory into registers, each wave its own tiles, K of the next tile on its way while this one's second half is computed and V behind it: up to
+// 16 KB in flight per wave.  All key tiles of the batch laid end to end are cut into equal parts, one per workgroup, wherever sequences and heads
+// begin and end; a column tile whose keys lie in several parts is joined by kv_join_kernel.
+constexpr int FEW_WAVES = 4, FEW_LEAST = 4;           // FEW_LEAST: tiles that are worth a workgroup
 
-__device__ __forceinline__ float code_at(uint32_t w, int byte) { return __builtin_amdgcn_cvt_f32_fp8((int)(w >> (8 * byte)), 0); }
+struct FewPart {
+    int64_t total;
+    int wgs;
+    __device__ __forceinline__ int64_t begin(int w) const { return total * w / wgs; }
+    __device__ __forceinline__ int of(int64_t f) const {           // the workgroup with tile f
+        int w = (int)(f * wgs / total);
+        while (begin(w + 1) <= f) ++w;
+        while (begin(w) > f) --w;
+        return w;
+    }
+};
+template <int COLS>
+__device__ __forceinline__ FewPart few_parts(const AttendArgs& a, int wgs) {
+    FewPart p;
+    p.total = kv_total<COLS>(a);
+    p.wgs = (int)max((int64_t)1, min((int64_t)wgs, (p.total + FEW_LEAST - 1) / FEW_LEAST));
+    return p;
+}
+
+// One column tile of 32 over key tiles [t0, t1), of which each wave takes every FEW_WAVES-th: its own result.  Tiles that every column sees whole
+// come first, one after the other without a break in the loads; then those with an end, a hole in the page table or a power that is none, if there are any.
+template <int HD>
+__device__ __forceinline__ void few_sweep(const AttendArgs& a, const KvSeq& q, int h, int c, int t0, int t1, const bf16x8 (*sq)[64], KvState<HD>& st) {
+    constexpr int KJ = HD / 32, DT = HD / 32, GB = 16 * HD, STEP = FEW_WAVES;
+    const int lane = threadIdx.x & 63, lj = lane & 31, lg = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const KvColumn col = kv_column(a, q, h, 32 * c + lj);
+    const int end_least = __builtin_amdgcn_readlane(col.end, 0), end_most = __builtin_amdgcn_readlane(col.end, min(32, q.n * a.times - 32 * c) - 1);
+    t1 = min(t1, (max(end_most, 0) + KV_TILE - 1) / KV_TILE);
+    st.clear();
+    // Groups are looked up for 16 tiles at a time, t, t + STEP, ...: lane l has group l & 3 of the (l >> 2)-th.
+    auto where = [&](int t) __attribute__((always_inline)) {
+        const int64_t p = (int64_t)(t + STEP * (lane >> 2)) * KV_TILE + 16 * (lane & 3);
+        return p < q.len ? kv_group(a.c, q.b, h, (int)p) : -1;
+    };
+    auto powers = [&](int g) __attribute__((always_inline)) { return g < 0 ? 0x7f7fu : (uint32_t)*(const uint16_t*)(a.c.scales + 2 * (int64_t)g); };
+    auto tiles = [&](int t) __attribute__((always_inline)) {                     // bit 4 i: there is an i-th one
+        const int m = (t1 - t + STEP - 1) / STEP;
+        return 0x1111111111111111ull & (m >= 16 ? ~0ull : (1ull << 4 * max(m, 0)) - 1);
+    };
+    auto odd_ones = [&](int t, int g, uint32_t p) __attribute__((always_inline)) {
+        const bool plain = g >= 0 && (p & 255u) != 255u && p >> 8 != 255u && (t + STEP * (lane >> 2)) * KV_TILE + 16 * (lane & 3) + 16 <= end_least;
+        uint64_t m = __ballot(!plain);
+        m |= m >> 2;
+        return (m | m >> 1) & tiles(t);
+    };
+    const int slot = (lj & 3) + 4 * (lj >> 3), kg = (lj >> 2) & 1;
+    uint32x4 kq[2][KJ], vq[2][DT];
+    uint32_t ksc[2], vsc[2];
+    auto load_k = [&](int g, uint32_t p, int nth) __attribute__((always_inline)) {
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+            const int from = nth * 4 + 2 * mt + kg;
+            ksc[mt] = __shfl(p, from) & 255u;
+            const uint8_t* const at = a.c.k + (int64_t)max(__shfl(g, from), 0) * GB + lg * 256 + slot * 16;
+#pragma unroll
+            for (int j = 0; j < KJ; ++j) kq[mt][j] = *(const uint32x4*)(at + j * 512);
+        }
+    };
+    auto load_v = [&](int g, uint32_t p, int nth) __attribute__((always_inline)) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int from = nth * 4 + 2 * s + lg;
+            vsc[s] = __shfl(p, from) >> 8;
+            const uint8_t* const at = a.c.v + (int64_t)max(__shfl(g, from), 0) * GB + lj * 16;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) vq[s][d] = *(const uint32x4*)(at + d * 512);
+        }
+    };
+    floatx16 s[2];
+    bf16x8 pf[4];
+    auto scores = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[mt][v] = 0.0f;
+        const float f0 = kv_power(ksc[0]), f1 = kv_power(ksc[1]);
+#pragma unroll
+        for (int k = 0; k < 2 * KJ; ++k) {
+            const bf16x8 qf = sq[k][lane];
+            s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kv_wide(kq[0][k >> 1][2 * (k & 1)], kq[0][k >> 1][2 * (k & 1) + 1], f0), qf, s[0], 0, 0, 0);
+            s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kv_wide(kq[1][k >> 1][2 * (k & 1)], kq[1][k >> 1][2 * (k & 1) + 1], f1), qf, s[1], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);             // (conversions far ahead of their MFMAs would only hold registers)
+        }
+    };
+    auto values = [&]() __attribute__((always_inline)) {
+        const float f0 = kv_power(vsc[0]), f1 = kv_power(vsc[1]);
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                st.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kv_wide(vq[ks >> 1][d][2 * (ks & 1)], vq[ks >> 1][d][2 * (ks & 1) + 1], ks >> 1 ? f1 : f0), pf[ks], st.o[d], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    };
+
+    int t = t0 + wave, odd_from = t1, odd_to = 0;          // the groups' 16 tiles begin at t; of those with odd tiles, the first and the last
+    if (t < t1) {
+        int g = where(t), t_next = t + 16 * STEP, g_next = where(t_next);
+        uint32_t p = powers(g), p_next = 0;
+        bool looked = false;                               // p_next is that of g_next
+        uint64_t odd = odd_ones(t, g, p), todo = tiles(t) & ~odd;
+        auto next = [&]() __attribute__((always_inline)) {
+            for (;;) {
+                if (odd) {
+                    odd_from = min(odd_from, t);
+                    odd_to = t;
+                    odd = 0;
+                }
+                if (todo) break;
+                if (t_next >= t1) return -1;
+                p = looked ? p_next : powers(g_next);
+                g = g_next;
+                t = t_next;
+                t_next += 16 * STEP;
+                g_next = where(t_next);
+                looked = false;
+                odd = odd_ones(t, g, p);
+                todo = tiles(t) & ~odd;
+            }
+            const int nth = __builtin_ctzll(todo) >> 2;
+            todo &= todo - 1;
+            if (!looked && !(todo >> 32)) {                // its first half is done: the table's entries are there by now
+                p_next = powers(g_next);
+                looked = true;
+            }
+            return nth;
+        };
+        int nth = next();
+        if (nth >= 0) {
+            load_k(g, p, nth);
+            load_v(g, p, nth);
+        }
+        while (nth >= 0) {
+            scores();
+            nth = next();
+            if (nth >= 0) load_k(g, p, nth);
+            __builtin_amdgcn_sched_barrier(0);
+            kv_softmax<HD>(st, s, a.c2, pf);
+            __builtin_amdgcn_sched_barrier(0);
+            values();
+            if (nth >= 0) load_v(g, p, nth);
+        }
+    }
+    for (t = odd_from; t <= odd_to; t += 16 * STEP) {
+        const int g = where(t);
+        const uint32_t p = powers(g);
+        for (uint64_t odd = odd_ones(t, g, p); odd; odd &= odd - 1) {
+            const int nth = __builtin_ctzll(odd) >> 2, k0 = (t + STEP * nth) * KV_TILE;
+            load_k(g, p, nth);
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt) {
+                const bool none = ksc[mt] == 255u;
+                ksc[mt] = none ? 127u : ksc[mt];
+#pragma unroll
+                for (int j = 0; j < KJ; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) kq[mt][j][e] = none ? 0x7f7f7f7fu : kq[mt][j][e];
+            }
+            scores();
+            __builtin_amdgcn_sched_barrier(0);
+            int rel[2], held[2];           // of the lane's 16 keys of a half: how many its column sees, how many there are (S^T's registers and V's tokens are the same group)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const bool there = __shfl(g, nth * 4 + 2 * i + lg) >= 0;
+                const int from = k0 + 32 * i + 16 * lg;
+                held[i] = there ? min(max(q.len - from, 0), 16) : 0;
+                rel[i] = there ? min(max(col.end - from, 0), 16) : 0;
+            }
+            kv_mask(s, rel);
+            kv_softmax<HD>(st, s, a.c2, pf);
+            __builtin_amdgcn_sched_barrier(0);
+            load_v(g, p, nth);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const bool none = vsc[i] == 255u;
+                vsc[i] = none || held[i] == 0 ? 127u : vsc[i];
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int b = min(max(held[i] - 4 * w, 0), 4);
+                    const uint32_t keep = b == 4 ? ~0u : (1u << (8 * b)) - 1u;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) vq[i][d][w] = (none ? 0x7f7f7f7fu : vq[i][d][w]) & keep;
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            uint32_t nans = 0;
+#pragma unroll
+            for (int i = 0; i < 2 * DT * 4; ++i) nans |= kv_perhaps_nan(vq[i / (DT * 4)][i / 4 % DT][i & 3]);
+            if (__any((nans & 0x80808080u) != 0)) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    floatx16 hits;
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) hits[v] = 0.0f;
+#pragma unroll
+                    for (int ks = 0; ks < 4; ++ks) {
+                        const uint32_t lo = vq[ks >> 1][d][2 * (ks & 1)], hi = vq[ks >> 1][d][2 * (ks & 1) + 1];
+                        const uint32_t n_lo = kv_nan_codes(lo), n_hi = kv_nan_codes(hi);
+                        vq[ks >> 1][d][2 * (ks & 1)] = kv_without_nan(lo, n_lo);
+                        vq[ks >> 1][d][2 * (ks & 1) + 1] = kv_without_nan(hi, n_hi);
+                        hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kv_wide(kv_ones(n_lo), kv_ones(n_hi), 1.0f), kv_seen(rel[ks >> 1], ks & 1), hits, 0, 0, 0);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    kv_spread_nan<HD>(st, d, hits);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            values();
+        }
+    }
+}
 
 template <int HD>
-__global__ __launch_bounds__(64) void kv_attend_kernel(AttendArgs a) {
-    __shared__ float sq[HD], sp[64];
-    const int lane = threadIdx.x, row = blockIdx.x, head = blockIdx.y, h = head / a.times, B = a.c.n_seqs;
-    int b = -1;
-    for (int base = 0; base < B; base += 64) {
-        const int i = base + lane;
-        b += __popcll(__ballot(i < B && a.cu[i] <= row));
-    }
-    if (b < 0 || row >= a.cu[b + 1]) return;
-    const int start = kv_clamped(a.cu[b], 0, a.n_tokens), n = kv_clamped(a.cu[b + 1], start, a.n_tokens) - start;
-    const int len = kv_clamped(a.lens[b], 0, a.c.capacity);
-    const int end = a.causal ? min(len, len - n + (row - start) + 1) : len;          // keys [0, end) are seen
-    for (int d = lane; d < HD; d += 64) sq[d] = (float)a.q[(int64_t)row * a.q_row + head * a.q_head + d];
-    __syncthreads();
-    float m = -INFINITY, l = 0.0f, o[HD / 64] = {};
-    for (int k0 = 0; k0 < end; k0 += 64) {
-        const int key = k0 + lane, g = key < end ? kv_group(a.c, b, h, key & ~15) : -1;
-        float s = -INFINITY;
-        if (g >= 0) {
-            const uint8_t* const p = a.c.k + (int64_t)g * (16 * HD) + (key & 15) * 16;
-            s = 0.0f;
-            for (int c = 0; c < HD / 16; ++c) {
-                const uint32x4 w = *(const uint32x4*)(p + c * 256);
-                for (int e = 0; e < 16; ++e) s = fmaf(code_at(w[e / 4], e & 3), sq[c * 16 + e], s);
+__global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attend_few_kernel(AttendArgs a) {
+    constexpr int DT = HD / 32;
+    __shared__ __attribute__((aligned(16))) float so[FEW_WAVES][DT * 4][64][4];
+    __shared__ float sm[FEW_WAVES][32][2];
+    __shared__ bf16x8 sq[HD / 16][64];                      // query fragments, the same for all waves
+    const int lane = threadIdx.x & 63, lj = lane & 31, lg = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = blockIdx.x;
+    const FewPart parts = few_parts<32>(a, gridDim.x);
+    if (w >= parts.wgs || parts.total == 0) return;
+    int64_t f = parts.begin(w);
+    const int64_t f1 = parts.begin(w + 1);
+    while (f < f1) {
+        const KvSeq q = kv_find<32>(a, f);
+        const int64_t q_end = q.first + (int64_t)q.ct * a.c.heads * q.tiles;
+        while (f < f1 && f < q_end) {
+            const int unit = (int)((f - q.first) / q.tiles), t0 = (int)((f - q.first) % q.tiles), t1 = (int)min((int64_t)q.tiles, t0 + (f1 - f));
+            const int h = unit / q.ct, c = unit % q.ct;
+            const KvColumn col = kv_column(a, q, h, 32 * c + lj);
+            for (int k = wave; k < HD / 16; k += FEW_WAVES)
+                sq[k][lane] = *(const bf16x8*)(a.q + (int64_t)col.row * a.q_row + (int64_t)col.head * a.q_head + 32 * (k >> 1) + 16 * lg + 8 * (k & 1));
+            __syncthreads();
+            KvState<HD> st;
+            few_sweep<HD>(a, q, h, c, t0, t1, sq, st);
+            const float l = st.l + __shfl_xor(st.l, 32);
+#pragma unroll
+            for (int i = 0; i < DT * 4; ++i)
+                *(floatx4*)so[wave][i][lane] = floatx4{st.o[i / 4][i % 4 * 4], st.o[i / 4][i % 4 * 4 + 1], st.o[i / 4][i % 4 * 4 + 2], st.o[i / 4][i % 4 * 4 + 3]};
+            if (lg == 0) {
+                sm[wave][lj][0] = st.mc;
+                sm[wave][lj][1] = l;
             }
-            s = __builtin_ldexpf(s, (int)a.c.scales[2 * (int64_t)g] - 127) * a.c2;
-        }
-        float hi = s;
-        for (int off = 32; off; off >>= 1) hi = fmaxf(hi, __shfl_xor(hi, off));
-        const float m_new = fmaxf(m, hi);
-        const bool none = m_new == -INFINITY;
-        const float f = none ? 1.0f : exp2f(m - m_new), pj = s == -INFINITY ? 0.0f : exp2f(s - (none ? 0.0f : m_new));      // (NaN comes through)
-        float sum = pj;
-        for (int off = 32; off; off >>= 1) sum += __shfl_xor(sum, off);
-        l = l * f + sum;
-        m = m_new;
-        sp[lane] = pj;
-        __syncthreads();
-        for (int i = 0; i < HD / 64; ++i) o[i] *= f;
-        for (int t = 0; t < 4; ++t) {
-            const int g2 = __shfl(g, t * 16);
-            if (g2 < 0) continue;
-            const int e2 = (int)a.c.scales[2 * (int64_t)g2 + 1] - 127;
-            for (int i = 0; i < HD / 64; ++i) {
-                const uint32x4 w = *(const uint32x4*)(a.c.v + (int64_t)g2 * (16 * HD) + (i * 64 + lane) * 16);
-                float x = 0.0f;
-                for (int e = 0; e < 16; ++e)
-                    if (k0 + t * 16 + e < end) x = fmaf(sp[t * 16 + e], code_at(w[e / 4], e & 3), x);
-                o[i] += __builtin_ldexpf(x, e2);
+            __syncthreads();
+            float m = kNoRef, sum = 0.0f, k[FEW_WAVES];
+#pragma unroll
+            for (int x = 0; x < FEW_WAVES; ++x) m = fmaxf(m, sm[x][lj][0]);
+#pragma unroll
+            for (int x = 0; x < FEW_WAVES; ++x) {
+                k[x] = __builtin_amdgcn_exp2f(sm[x][lj][0] - m);
+                sum = fmaf(sm[x][lj][1], k[x], sum);
             }
+            const bool whole = t0 == 0 && t1 == q.tiles;
+            const int at = 2 * w + (t0 == 0);
+            const float inv = kv_inverse(sum);
+            for (int i = wave; i < DT * 4; i += FEW_WAVES) {
+                floatx4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int x = 0; x < FEW_WAVES; ++x) {
+                    const floatx4 p = *(const floatx4*)so[x][i][lane];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = fmaf(p[e], k[x], v[e]);
+                }
+                const int d = 8 * i + 4 * lg;               // i = 4 dt + v / 4
+                if (!col.mine) continue;
+                if (whole) {
+                    bf16x4 r;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) r[e] = (bf16)(v[e] * inv);
+                    *(bf16x4*)(a.o + (int64_t)col.row * a.o_row + (int64_t)col.head * a.o_head + d) = r;
+                } else {
+                    *(floatx4*)(a.part_o + ((int64_t)at * 32 + lj) * HD + d) = v;
+                }
+            }
+            if (!whole && col.mine && wave == 0 && lg == 0) *(float2*)(a.part_ml + ((int64_t)at * 32 + lj) * 2) = make_float2(m, sum);
+            __syncthreads();
+            f += t1 - t0;
         }
-        __syncthreads();
     }
-    for (int i = 0; i < HD / 64; ++i) a.o[(int64_t)row * a.o_row + head * a.o_head + i * 64 + lane] = (bf16)(l == 0.0f ? 0.0f : o[i] / l);
+}
+
+// Joins the parts of the column tiles that have several: a workgroup per column tile, a lane per four dims of a column.
+template <int HD>
+__global__ __launch_bounds__(256) void kv_join_kernel(AttendArgs a, int wgs) {
+    const FewPart parts = few_parts<32>(a, wgs);
+    if (parts.total == 0) return;
+    // the (blockIdx.x)-th column tile: sequences in order, then heads
+    int64_t before = 0;
+    KvSeq q = {};
+    int unit = -1;
+    for (int base = 0; base < a.c.n_seqs; base += 64) {
+        const KvScan<32> s(a, base);
+        const int lane = threadIdx.x & 63;
+        int units = s.col_tiles(a) * a.c.heads;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(units, o);
+            units += lane >= o ? x : 0;
+        }
+        const int want = (int)blockIdx.x - unit - 1;           // unit + 1: column tiles of the sequences before base
+        const uint64_t m = __ballot(want < units);
+        if (m) {
+            const int l = __builtin_ctzll(m);
+            q = s.pick(a, base, before, l);
+            unit = want - (__builtin_amdgcn_readlane(units, l) - q.ct * a.c.heads);
+            goto found;
+        }
+        unit += __builtin_amdgcn_readlane(units, 63);
+        before += s.all();
+    }
+    return;
+found:
+    const int64_t f0 = q.first + (int64_t)unit * q.tiles;
+    const int w0 = parts.of(f0), w1 = parts.of(f0 + q.tiles - 1);
+    if (w0 == w1) return;
+    const int h = unit / q.ct, c = unit % q.ct, cols = min(32, q.n * a.times - 32 * c);
+    const int first = 2 * w0 + 1;
+    for (int i = threadIdx.x; i < cols * (HD / 4); i += 256) {
+        const int lj = i / (HD / 4), d = i % (HD / 4) * 4;
+        float m = kNoRef, sum = 0.0f;
+        for (int w = w0; w <= w1; ++w) m = fmaxf(m, a.part_ml[((int64_t)(w == w0 ? first : 2 * w) * 32 + lj) * 2]);
+        floatx4 v = {0.f, 0.f, 0.f, 0.f};
+        for (int w = w0; w <= w1; ++w) {
+            const int64_t at = (int64_t)(w == w0 ? first : 2 * w) * 32 + lj;
+            const float2 ml = *(const float2*)(a.part_ml + at * 2);
+            const float k = __builtin_amdgcn_exp2f(ml.x - m);
+            sum = fmaf(ml.y, k, sum);
+            const floatx4 p = *(const floatx4*)(a.part_o + at * HD + d);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = fmaf(p[e], k, v[e]);
+        }
+        const float inv = kv_inverse(sum);
+        const KvColumn col = kv_column(a, q, h, 32 * c + lj);
+        bf16x4 r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = (bf16)(v[e] * inv);
+        *(bf16x4*)(a.o + (int64_t)col.row * a.o_row + (int64_t)col.head * a.o_head + d) = r;
+    }
 }
 
 const char* query_bad(const cf_kv_cache* c, const cf_kv_query* x) {
@@ -87,13 +361,33 @@ const char* query_bad(const cf_kv_cache* c, const cf_kv_query* x) {
     return nullptr;
 }
 
+constexpr int FEW_WGS = 512;           // two on each CU
+
+struct AttendPlan {
+    int64_t units;                     // column tiles of all sequences and key heads, at most
+    uint64_t slots;                    // partial results of 32 columns
+    uint64_t ml_offset, bytes;         // of the workspace
+};
+const char* attend_plan(const cf_kv_cache* c, const cf_kv_query* x, AttendPlan* p) {
+    const int64_t times = x->heads / c->heads, cols = (int64_t)x->n_tokens * times;
+    if (cols > 0x7fffffff - 4096) return "too many queries";
+    p->units = (cols / 32 + std::min(c->n_seqs, x->n_tokens)) * c->heads;
+    if (p->units > 0x7fffffff) return "too many queries";
+    p->slots = 2 * FEW_WGS;
+    p->ml_offset = p->slots * 32 * c->head_dim * 4;
+    p->bytes = p->ml_offset + p->slots * 32 * 2 * 4;
+    return nullptr;
+}
+
 }  // namespace
 
 extern "C" int cf_kv_attention_workspace(const cf_kv_cache* cache, const cf_kv_query* x, uint64_t* bytes) {
     if (const char* bad = kv_bad(cache)) return cf_fail(nullptr, CF_ERR_ARG, "kv_attention_workspace: %s", bad);
     if (const char* bad = query_bad(cache, x)) return cf_fail(nullptr, CF_ERR_ARG, "kv_attention_workspace: %s", bad);
     if (!bytes) return cf_fail(nullptr, CF_ERR_ARG, "kv_attention_workspace: null result");
-    *bytes = 0;
+    AttendPlan p;
+    if (const char* bad = attend_plan(cache, x, &p)) return cf_fail(nullptr, CF_ERR_ARG, "kv_attention_workspace: %s", bad);
+    *bytes = p.bytes;
     return CF_OK;
 }
 
@@ -115,9 +409,20 @@ extern "C" int cf_kv_attention(const cf_kv_cache* cache, const cf_kv_query* x, v
     a.n_tokens = x->n_tokens; a.heads = x->heads; a.times = x->heads / cache->heads;
     a.causal = x->causal != 0;
     a.c2 = x->scale * 1.4426950408889634f;
-    const dim3 grid((unsigned)x->n_tokens, (unsigned)x->heads);
-    if (cache->head_dim == 128) hipLaunchKernelGGL(kv_attend_kernel<128>, grid, dim3(64), 0, (hipStream_t)stream, a);
-    else hipLaunchKernelGGL(kv_attend_kernel<64>, grid, dim3(64), 0, (hipStream_t)stream, a);
+    AttendPlan p;
+    if (const char* bad = attend_plan(cache, x, &p)) return cf_fail(nullptr, CF_ERR_ARG, "kv_attention: %s", bad);
+    if (!workspace || (uintptr_t)workspace % 256 || workspace_bytes < p.bytes)
+        return cf_fail(nullptr, CF_ERR_ARG, "kv_attention: a workspace of %llu bytes, 256-byte aligned, is needed", (unsigned long long)p.bytes);
+    a.part_o = (float*)workspace;
+    a.part_ml = (float*)((char*)workspace + p.ml_offset);
+    hipStream_t s = (hipStream_t)stream;
+    if (cache->head_dim == 128) {
+        hipLaunchKernelGGL(kv_attend_few_kernel<128>, dim3(FEW_WGS), dim3(64 * FEW_WAVES), 0, s, a);
+        hipLaunchKernelGGL(kv_join_kernel<128>, dim3((unsigned)p.units), dim3(256), 0, s, a, FEW_WGS);
+    } else {
+        hipLaunchKernelGGL(kv_attend_few_kernel<64>, dim3(FEW_WGS), dim3(64 * FEW_WAVES), 0, s, a);
+        hipLaunchKernelGGL(kv_join_kernel<64>, dim3((unsigned)p.units), dim3(256), 0, s, a, FEW_WGS);
+    }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? CF_OK : cf_fail(nullptr, CF_ERR_HIP, "kv_attention launch: %s", hipGetErrorString(e));
 }

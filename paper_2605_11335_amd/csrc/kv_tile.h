@@ -1,0 +1,212 @@
+// What the attention kernels over a paged 8-bit cache share: arguments, how a ragged batch is laid end to end, and the arithmetic of a tile of 64
+// keys against a wave's 32 columns.
+//
+// Columns.  The query rows of a sequence times the query heads of a key head, row after row, are the columns of that (sequence, key head); 32 of them
+// are a column tile of a wave.  As in attention.hip a wave works on the transposed problem, S^T = K Q^T and O^T = V^T P^T with 32x32x16 MFMAs: a
+// lane owns a column (lane & 31) and half of the keys (lane >> 5), softmax reference and row sum are per-lane scalars, and P^T is S^T repacked.
+//
+// Operands.  The order of the contracted index is free as long as both operands share it, and so is the key that a row of S^T stands for.  Both are
+// chosen so that a lane's part of K or V is 16 consecutive bytes of the cache, two k-steps' worth:
+//   S^T: lane group lg (0, 1) has dims 16 (2j + lg) + 8u + 0..7 at k-step 2j + u: K chunk 2j + lg of its key's group.
+//   Row r of S^T's half mt is key 32 mt + 16 ((r >> 2) & 1) + (r & 3) + 4 (r >> 3), so that register v of lane group lg is key 32 mt + 16 lg + v.
+//   O^T: lane group lg has keys 32 s + 16 lg + 8u + 0..7 at k-step 2s + u: V's 16 tokens of group 2s + lg, and S^T's registers 8u .. 8u + 7 of half s.
+#pragma once
+#include <math.h>
+
+#include "kv_cache.h"
+
+struct AttendArgs {
+    KvView c;
+    const bf16* q;
+    bf16* o;
+    int64_t q_row, q_head, o_row, o_head;
+    const int32_t *cu, *lens;
+    int32_t n_tokens, heads, times;        // times: query heads per key head
+    int32_t causal;
+    float c2;                              // scale * log2(e)
+    float* part_o;                         // results of parts of a column tile's keys: [slot][column][head_dim], then
+    float* part_ml;                        // [slot][column][2]: reference (base 2) and sum of the weights
+};
+
+constexpr int KV_TILE = 64;                // keys
+
+// A sequence of the batch, its column tiles and key tiles.  `first`: where its tiles begin when all (sequence, key head, column tile)s' key
+// tiles are laid end to end.
+struct KvSeq {
+    int b, start, n, len, ct, tiles;
+    int64_t first;
+};
+
+// values that all lanes agree on, in scalar registers
+__device__ __forceinline__ int64_t kv_lane64(int64_t x, int lane) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, lane));
+}
+// The sequence of each lane, i = base + lane, and the inclusive sum of the key tiles up to it.
+template <int COLS>
+struct KvScan {
+    int start, n, len;
+    int64_t upto;
+    __device__ __forceinline__ int col_tiles(const AttendArgs& a) const { return (n * a.times + COLS - 1) / COLS; }
+    // an empty sequence has a tile, too, whose columns have to be set to zero
+    __device__ __forceinline__ static int key_tiles(int len) { return max(1, (len + KV_TILE - 1) / KV_TILE); }
+    __device__ __forceinline__ KvScan(const AttendArgs& a, int base) {
+        const int lane = threadIdx.x & 63, i = base + lane;
+        start = n = len = 0;
+        if (i < a.c.n_seqs) {
+            start = kv_clamped(a.cu[i], 0, a.n_tokens);
+            n = kv_clamped(a.cu[i + 1], start, a.n_tokens) - start;
+            len = kv_clamped(a.lens[i], 0, a.c.capacity);
+        }
+        upto = (int64_t)col_tiles(a) * a.c.heads * key_tiles(len);
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int64_t x = __shfl_up((long long)upto, o);
+            upto += lane >= o ? x : 0;
+        }
+    }
+    __device__ __forceinline__ int64_t all() const { return kv_lane64(upto, 63); }
+    __device__ __forceinline__ KvSeq pick(const AttendArgs& a, int base, int64_t before, int lane) const {
+        KvSeq s;
+        s.b = base + lane;
+        s.start = __builtin_amdgcn_readlane(start, lane);
+        s.n = __builtin_amdgcn_readlane(n, lane);
+        s.len = __builtin_amdgcn_readlane(len, lane);
+        s.ct = (s.n * a.times + COLS - 1) / COLS;
+        s.tiles = key_tiles(s.len);
+        s.first = before + kv_lane64(upto, lane) - (int64_t)s.ct * a.c.heads * s.tiles;
+        return s;
+    }
+};
+template <int COLS>
+__device__ __forceinline__ int64_t kv_total(const AttendArgs& a) {
+    int64_t t = 0;
+    for (int base = 0; base < a.c.n_seqs; base += 64) t += KvScan<COLS>(a, base).all();
+    return t;
+}
+// The sequence with tile f, 0 <= f < kv_total.
+template <int COLS>
+__device__ __forceinline__ KvSeq kv_find(const AttendArgs& a, int64_t f) {
+    int64_t before = 0;
+    for (int base = 0;; base += 64) {
+        const KvScan<COLS> s(a, base);
+        const uint64_t m = __ballot(f < before + s.upto);
+        if (m) return s.pick(a, base, before, __builtin_ctzll(m));
+        before += s.all();
+    }
+}
+
+// A lane's column of a column tile.
+struct KvColumn {
+    int row, head, end;                    // query row, query head, keys [0, end) are seen
+    bool mine;                             // a column, not padding (which repeats the last one)
+};
+__device__ __forceinline__ KvColumn kv_column(const AttendArgs& a, const KvSeq& s, int h, int col) {
+    const int cols = s.n * a.times, c = min(col, cols - 1), i = c / a.times;
+    return {s.start + i, h * a.times + (c - i * a.times), a.causal ? min(s.len, s.len - s.n + i + 1) : s.len, col < cols};
+}
+
+// ---- a tile
+constexpr float kNoRef = -3.402823466e38f;        // reference of a column before its first score
+template <int HD>
+struct KvState {
+    floatx16 o[HD / 32];                   // O^T: register v of dt = dim 32 dt + (v & 3) + 8 (v >> 2) + 4 lg
+    float mc, l;                           // reference, base 2; sum of the weights of this lane's keys
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) o[d][v] = 0.0f;
+        mc = kNoRef;
+        l = 0.0f;
+    }
+};
+
+// eight codes times a power of two, exactly (bf16 has the bits)
+__device__ __forceinline__ bf16x8 kv_wide(uint32_t lo, uint32_t hi, float scale) {
+    uint32x4 r;
+    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false));
+    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true));
+    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false));
+    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true));
+    return __builtin_bit_cast(bf16x8, r);
+}
+__device__ __forceinline__ float kv_power(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Scores of keys that a column does not see become -inf: rel[mt] = how many of the lane's 16 keys of half mt it sees.
+__device__ __forceinline__ void kv_mask(floatx16 (&s)[2], const int (&rel)[2]) {
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s[mt][v] = v < rel[mt] ? s[mt][v] : -INFINITY;
+}
+
+// Weights of a tile: P^T in bf16 as the second contraction takes it, and the sum of the weights as rounded.  The reference is not the
+// running maximum: softmax does not depend on it, and fp32 and bf16 are as exact at 2^19 as at 1.  It stays where it is as long as a lane's 32 weights
+// add up to less than 2^20, which the sum, needed anyway, tells; else it moves to the largest score (always in a column's first tile,
+// where weights against kNoRef are infinite), and what has been summed up is brought to it.
+template <int HD>
+__device__ __forceinline__ void kv_softmax(KvState<HD>& st, const floatx16 (&s)[2], float c2, bf16x8 (&pf)[4]) {
+    float psum;
+    auto weigh = [&]() __attribute__((always_inline)) {
+        float ps[4] = {0.f, 0.f, 0.f, 0.f};
+        bf16x2 ones;
+        ones[0] = ones[1] = (bf16)1.0f;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                bf16x2 pp;
+                pp[0] = (bf16)__builtin_amdgcn_exp2f(fmaf(s[ks >> 1][8 * (ks & 1) + e], c2, -st.mc));
+                pp[1] = (bf16)__builtin_amdgcn_exp2f(fmaf(s[ks >> 1][8 * (ks & 1) + e + 1], c2, -st.mc));
+                pf[ks][e] = pp[0];
+                pf[ks][e + 1] = pp[1];
+                ps[(e >> 1) & 3] = __builtin_amdgcn_fdot2_f32_bf16(pp, ones, ps[(e >> 1) & 3], false);
+            }
+        psum = (ps[0] + ps[1]) + (ps[2] + ps[3]);
+    };
+    weigh();
+    if (__any(!(psum < 1048576.0f))) {
+        float mx = s[0][0];
+#pragma unroll
+        for (int v = 1; v < 32; ++v) mx = fmaxf(mx, s[v >> 4][v & 15]);
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float mc = fmaxf(st.mc, mx * c2), f = __builtin_amdgcn_exp2f(st.mc - mc);
+        st.mc = mc;
+        st.l *= f;
+#pragma unroll
+        for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) st.o[d][v] *= f;
+        weigh();
+    }
+    st.l += psum;
+}
+
+// A NaN among values reaches the columns that see its key and no others, though their weight of zero would carry it there: NaN codes are
+// taken out before the second contraction, and a contraction of its own, of which codes were NaN with which keys are seen, says which sums they belong to.
+__device__ __forceinline__ uint32_t kv_nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }        // bit 7 of each NaN
+// A bit 7 where there is a NaN, and perhaps where there is none.  (Another formula on purpose: the compiler would keep the results of the same one in
+// 64 registers until they are used again.)
+__device__ __forceinline__ uint32_t kv_perhaps_nan(uint32_t w) { return (~w & 0x7f7f7f7fu) - 0x01010101u; }
+__device__ __forceinline__ uint32_t kv_without_nan(uint32_t w, uint32_t nans) { return w & ~((nans << 1) - (nans >> 7)); }
+__device__ __forceinline__ uint32_t kv_ones(uint32_t nans) { return (nans >> 7) * 0x38u; }                                          // the code of 1
+__device__ __forceinline__ bf16x8 kv_seen(int rel, int u) {
+    bf16x8 r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = 8 * u + e < rel ? (bf16)1.0f : (bf16)0.0f;
+    return r;
+}
+template <int HD>
+__device__ __forceinline__ void kv_spread_nan(KvState<HD>& st, int d, const floatx16& hits) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) st.o[d][v] = hits[v] > 0.0f ? __uint_as_float(0x7fc00000u) : st.o[d][v];
+}
+
+// Two partial results of a column, each against its own reference, brought to the higher one.
+struct KvJoin {
+    float m, before, part;
+    __device__ __forceinline__ KvJoin(float m0, float m1) : m(fmaxf(m0, m1)), before(__builtin_amdgcn_exp2f(m0 - m)), part(__builtin_amdgcn_exp2f(m1 - m)) {}
+    __device__ __forceinline__ float operator()(float x0, float x1) const { return fmaf(x1, part, x0 * before); }
+};
+// What divides: 0 where a column has seen nothing.
+__device__ __forceinline__ float kv_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
