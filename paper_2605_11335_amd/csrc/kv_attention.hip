@@ -13,26 +13,7 @@ namespace {
 // memory into registers, each wave its own tiles, K of the next tile on its way while this one's second half is computed and V behind it: up to
 // 16 KB in flight per wave.  All key tiles of the batch laid end to end are cut into equal parts, one per workgroup, wherever sequences and heads
 // begin and end; a column tile whose keys lie in several parts is joined by kv_join_kernel.
-constexpr int FEW_WAVES = 4, FEW_LEAST = 4;           // FEW_LEAST: tiles that are worth a workgroup
-
-struct FewPart {
-    int64_t total;
-    int wgs;
-    __device__ __forceinline__ int64_t begin(int w) const { return total * w / wgs; }
-    __device__ __forceinline__ int of(int64_t f) const {           // the workgroup with tile f
-        int w = (int)(f * wgs / total);
-        while (begin(w + 1) <= f) ++w;
-        while (begin(w) > f) --w;
-        return w;
-    }
-};
-template <int COLS>
-__device__ __forceinline__ FewPart few_parts(const AttendArgs& a, int wgs) {
-    FewPart p;
-    p.total = kv_total<COLS>(a);
-    p.wgs = (int)max((int64_t)1, min((int64_t)wgs, (p.total + FEW_LEAST - 1) / FEW_LEAST));
-    return p;
-}
+constexpr int FEW_WAVES = 4, FEW_LEAST = 4 * KV_TILE;           // FEW_LEAST: keys that are worth a workgroup
 
 // One column tile of 32 over key tiles [t0, t1), of which each wave takes every FEW_WAVES-th: its own result.  Tiles that every column sees whole
 // come first, one after the other without a break in the loads; then those with an end, a hole in the page table or a power that is none, if there are any.
@@ -234,22 +215,22 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attend_few_kernel(Attend
     __shared__ float sm[FEW_WAVES][32][2];
     __shared__ bf16x8 sq[HD / 16][64];                      // query fragments, the same for all waves
     const int lane = threadIdx.x & 63, lj = lane & 31, lg = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = blockIdx.x;
-    const FewPart parts = few_parts<32>(a, gridDim.x);
-    if (w >= parts.wgs || parts.total == 0) return;
-    int64_t f = parts.begin(w);
-    const int64_t f1 = parts.begin(w + 1);
+    const KvShares shares(kv_total<32>(a), gridDim.x, FEW_LEAST);
+    if (w >= shares.wgs || shares.total == 0) return;
+    int64_t f = shares.begin(w);
+    const int64_t f1 = shares.begin(w + 1);
     while (f < f1) {
         const KvSeq q = kv_find<32>(a, f);
-        const int64_t q_end = q.first + (int64_t)q.ct * a.c.heads * q.tiles;
+        const int64_t q_end = q.first + q.head() * a.c.heads;
         while (f < f1 && f < q_end) {
-            const int unit = (int)((f - q.first) / q.tiles), t0 = (int)((f - q.first) % q.tiles), t1 = (int)min((int64_t)q.tiles, t0 + (f1 - f));
-            const int h = unit / q.ct, c = unit % q.ct;
+            const KvPiece p = kv_piece<32>(a, q, f, f1);
+            const int h = p.h, c = p.c;
             const KvColumn col = kv_column(a, q, h, 32 * c + lj);
             for (int k = wave; k < HD / 16; k += FEW_WAVES)
                 sq[k][lane] = *(const bf16x8*)(a.q + (int64_t)col.row * a.q_row + (int64_t)col.head * a.q_head + 32 * (k >> 1) + 16 * lg + 8 * (k & 1));
             __syncthreads();
             KvState<HD> st;
-            few_sweep<HD>(a, q, h, c, t0, t1, sq, st);
+            few_sweep<HD>(a, q, h, c, p.t0, p.t1, sq, st);
             const float l = st.l + __shfl_xor(st.l, 32);
 #pragma unroll
             for (int i = 0; i < DT * 4; ++i)
@@ -267,20 +248,19 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attend_few_kernel(Attend
                 k[x] = __builtin_amdgcn_exp2f(sm[x][lj][0] - m);
                 sum = fmaf(sm[x][lj][1], k[x], sum);
             }
-            const bool whole = t0 == 0 && t1 == q.tiles;
-            const int at = 2 * w + (t0 == 0);
+            const int at = 2 * w + p.from_start;            // the share's first piece may begin inside a column tile, its last may end inside one
             const float inv = kv_inverse(sum);
             for (int i = wave; i < DT * 4; i += FEW_WAVES) {
                 floatx4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int x = 0; x < FEW_WAVES; ++x) {
-                    const floatx4 p = *(const floatx4*)so[x][i][lane];
+                    const floatx4 y = *(const floatx4*)so[x][i][lane];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = fmaf(p[e], k[x], v[e]);
+                    for (int e = 0; e < 4; ++e) v[e] = fmaf(y[e], k[x], v[e]);
                 }
                 const int d = 8 * i + 4 * lg;               // i = 4 dt + v / 4
                 if (!col.mine) continue;
-                if (whole) {
+                if (p.whole) {
                     bf16x4 r;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) r[e] = (bf16)(v[e] * inv);
@@ -289,68 +269,279 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attend_few_kernel(Attend
                     *(floatx4*)(a.part_o + ((int64_t)at * 32 + lj) * HD + d) = v;
                 }
             }
-            if (!whole && col.mine && wave == 0 && lg == 0) *(float2*)(a.part_ml + ((int64_t)at * 32 + lj) * 2) = make_float2(m, sum);
+            if (!p.whole && col.mine && wave == 0 && lg == 0) *(float2*)(a.part_ml + ((int64_t)at * 32 + lj) * 2) = make_float2(m, sum);
             __syncthreads();
-            f += t1 - t0;
+            f = p.next;
         }
     }
 }
 
-// Joins the parts of the column tiles that have several: a workgroup per column tile, a lane per four dims of a column.
-template <int HD>
-__global__ __launch_bounds__(256) void kv_join_kernel(AttendArgs a, int wgs) {
-    const FewPart parts = few_parts<32>(a, wgs);
-    if (parts.total == 0) return;
-    // the (blockIdx.x)-th column tile: sequences in order, then heads
+// ---------------------------------------------------------------------------------------------
+// Many columns: a workgroup of NW waves has 32 NW columns of a (sequence, key head) and goes through its share of the keys, tiles of 64 that all its
+// waves use.  Bound by the matrix cores and, nearly as much, by reading fragments from LDS.  Codes become bf16 once per workgroup, on their way into
+// LDS: a lane's 16 bytes are two fragments' worth (kv_tile.h), stored as the fragments lie, so that a fragment read is 1 KiB in order and
+// nothing has to be swizzled.  Tile t + 2 is on its way from memory and t + 1 is converted into the other buffer while t is computed.
+struct ManyFlags {
+    uint32_t held;                                     // tokens of each of the tile's groups, a byte each
+    uint32_t nan;                                      // t + 1 where a value of tile t was NaN and not every column sees the tile whole
+};
+template <int HD, int NW>
+struct ManyShared {
+    bf16x8 k[2][2][HD / 16][64], v[2][4][HD / 32][64];
+    uint16_t nan_of[2][4 * HD];                        // which of a V chunk's 16 tokens were NaN, in such a tile
+    ManyFlags flags[2];
+};
+
+template <int HD, int NW>
+__device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, int h, int c, int t0, int t1, ManyShared<HD, NW>& sh, KvState<HD>& st) {
+    constexpr int KS = HD / 16, DT = HD / 32, NT = 64 * NW, GB = 16 * HD;
+    constexpr int CHUNKS = 4 * HD, PER = CHUNKS >= NT ? CHUNKS / NT : 1;        // 16-byte chunks of a tile's K; of those and of V, a lane has PER
+    constexpr bool BOTH = CHUNKS >= NT;                                         // else half of the lanes have K, half V
+    static_assert(CHUNKS % NT == 0 || 2 * CHUNKS == NT, "");
+    const int tid = threadIdx.x, lane = tid & 63, lj = lane & 31, lg = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col0 = 32 * NW * c + 32 * wave, cols = min(32, q.n * a.times - col0);            // (cols <= 0: a wave without a column only copies)
+    const KvColumn col = kv_column(a, q, h, col0 + lj);
+    const int end_least = cols > 0 ? __builtin_amdgcn_readlane(col.end, 0) : 0x7fffffff, end_most = cols > 0 ? __builtin_amdgcn_readlane(col.end, cols - 1) : 0;
+    const int wg_least = a.causal ? min(q.len, q.len - q.n + 32 * NW * c / a.times + 1) : q.len;             // of all waves
+    st.clear();
+    if (t0 >= t1) return;
+    bf16x8 qf[KS];
+    {
+        const bf16* const p = a.q + (int64_t)col.row * a.q_row + (int64_t)col.head * a.q_head + 16 * lg;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) qf[k] = *(const bf16x8*)(p + 32 * (k >> 1) + 8 * (k & 1));
+    }
+    // ---- copies.  Chunk x of K or V: group x / HD of the tile, 16 bytes x % HD of it.
+    const bool has_k = BOTH || tid < CHUNKS, has_v = BOTH || tid >= CHUNKS;
+    const int x0 = BOTH ? tid : tid % CHUNKS;
+    int g_of[PER];                                     // groups of the tile that is looked up
+    uint32_t pw[PER];                                  // powers of the one in flight
+    uint32_t held[PER];                                // its tokens there are
+    uint32x4 kr[PER], vr[PER];
+    auto look_up = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int64_t p = (int64_t)t * KV_TILE + 16 * ((i * NT + x0) / HD);
+            g_of[i] = t < t1 && p < q.len ? kv_group(a.c, q.b, h, (int)p) : -1;
+        }
+    };
+    auto fetch = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int x = i * NT + x0, g = max(g_of[i], 0);
+            held[i] = g_of[i] < 0 ? 0 : min(max(q.len - (t * KV_TILE + 16 * (x / HD)), 0), 16);
+            pw[i] = *(const uint16_t*)(a.c.scales + 2 * (int64_t)g);
+            if (has_k) kr[i] = *(const uint32x4*)(a.c.k + (int64_t)g * GB + (x % HD) * 16);
+            if (has_v) vr[i] = *(const uint32x4*)(a.c.v + (int64_t)g * GB + (x % HD) * 16);
+        }
+    };
+    auto convert = [&](int t, int buf) __attribute__((always_inline)) {
+        const bool part = (t + 1) * KV_TILE > wg_least;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int x = i * NT + x0, grp = x / HD, r = x % HD;
+            uint32_t pk = pw[i] & 255u, pv = pw[i] >> 8;
+            if (__any(held[i] < 16 || pk == 255u || pv == 255u)) {
+                const bool nk = pk == 255u, nv = pv == 255u;
+                pk = nk || held[i] == 0 ? 127u : pk;
+                pv = nv || held[i] == 0 ? 127u : pv;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int b = min(max((int)held[i] - 4 * w, 0), 4);
+                    const uint32_t keep = b == 4 ? ~0u : (1u << (8 * b)) - 1u;
+                    kr[i][w] = nk ? 0x7f7f7f7fu : kr[i][w];
+                    vr[i][w] = (nv ? 0x7f7f7f7fu : vr[i][w]) & keep;
+                }
+            }
+            if (has_k) {
+                const int slot = r & 15, ch = r >> 4, row = (slot & 3) | (grp & 1) << 2 | (slot >> 2) << 3, to = row + 32 * (ch & 1);
+                const float f = kv_power(pk);
+                sh.k[buf][grp >> 1][ch & ~1][to] = kv_wide(kr[i][0], kr[i][1], f);
+                sh.k[buf][grp >> 1][ch | 1][to] = kv_wide(kr[i][2], kr[i][3], f);
+            }
+            if (has_v) {
+                if (part) {
+                    uint32_t m = 0;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const uint32_t nans = kv_nan_codes(vr[i][w]);
+                        vr[i][w] = kv_without_nan(vr[i][w], nans);
+                        m |= ((nans >> 7) * 0x10204080u >> 28) << (4 * w);          // four bits side by side
+                    }
+                    sh.nan_of[buf][x] = (uint16_t)m;
+                    if (m) sh.flags[buf].nan = (uint32_t)t + 1;
+                }
+                const int to = (r & 31) + 32 * (grp & 1);
+                const float f = kv_power(pv);
+                sh.v[buf][grp & ~1][r >> 5][to] = kv_wide(vr[i][0], vr[i][1], f);
+                sh.v[buf][grp | 1][r >> 5][to] = kv_wide(vr[i][2], vr[i][3], f);
+            }
+            if (has_k && r == 0) ((uint8_t*)&sh.flags[buf].held)[grp] = (uint8_t)held[i];
+        }
+    };
+    if (tid < 2) sh.flags[tid].nan = 0;
+    look_up(t0);
+    fetch(t0);
+    look_up(t0 + 1);
+    __syncthreads();                                   // the flags are cleared; what the buffers held before has been read
+    convert(t0, t0 & 1);
+    fetch(t0 + 1);
+    look_up(t0 + 2);
+    __syncthreads();
+    for (int t = t0; t < t1; ++t) {
+        const int buf = t & 1;
+        if (t + 1 < t1) convert(t + 1, buf ^ 1);
+        if (t + 2 < t1) fetch(t + 2);
+        look_up(t + 3);
+        if (t * KV_TILE < end_most) {
+            const uint32_t there = sh.flags[buf].held;
+            const bool nan = sh.flags[buf].nan == (uint32_t)t + 1;
+            const bool part = __builtin_amdgcn_readfirstlane(there) != 0x10101010u || (t + 1) * KV_TILE > end_least;
+            floatx16 s[2];
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) s[mt][v] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(sh.k[buf][0][k][lane], qf[k], s[0], 0, 0, 0);
+                s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(sh.k[buf][1][k][lane], qf[k], s[1], 0, 0, 0);
+            }
+            int rel[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) rel[i] = min((int)(there >> (8 * (2 * i + lg)) & 255u), min(max(col.end - (t * KV_TILE + 32 * i + 16 * lg), 0), 16));
+            if (part) kv_mask(s, rel);
+            __builtin_amdgcn_sched_barrier(0);
+            bf16x8 pf[4];
+            kv_softmax<HD>(st, s, a.c2, pf);
+            __builtin_amdgcn_sched_barrier(0);
+            if (__builtin_amdgcn_readfirstlane(nan)) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    floatx16 hits;
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) hits[v] = 0.0f;
+#pragma unroll
+                    for (int ks = 0; ks < 4; ++ks) {
+                        const uint32_t m = sh.nan_of[buf][(2 * (ks >> 1) + lg) * HD + 32 * d + lj] >> (8 * (ks & 1));
+                        bf16x8 was;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) was[e] = m >> e & 1u ? (bf16)1.0f : (bf16)0.0f;
+                        hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(was, kv_seen(rel[ks >> 1], ks & 1), hits, 0, 0, 0);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    kv_spread_nan<HD>(st, d, hits);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) st.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(sh.v[buf][ks][d][lane], pf[ks], st.o[d], 0, 0, 0);
+        }
+        __syncthreads();                               // tile t + 1 is in its buffer, that of t is free
+    }
+}
+
+constexpr int MANY_LEAST = 8 * KV_TILE;                // keys that are worth a workgroup
+template <int HD, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a) {
+    constexpr int DT = HD / 32, COLS = 32 * NW;
+    __shared__ ManyShared<HD, NW> sh;
+    const int lane = threadIdx.x & 63, lj = lane & 31, lg = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const KvShares shares(kv_total<COLS>(a), gridDim.x, MANY_LEAST);
+    if ((int)blockIdx.x >= shares.wgs || shares.total == 0) return;
+    const int w = (int)xcd_contiguous_id(blockIdx.x, shares.wgs);         // neighbours in the work, which share keys, on one XCD
+    int64_t f = shares.begin(w);
+    const int64_t f1 = shares.begin(w + 1);
+    while (f < f1) {
+        const KvSeq q = kv_find<COLS>(a, f);
+        const int64_t q_end = q.first + q.head() * a.c.heads;
+        while (f < f1 && f < q_end) {
+            const KvPiece p = kv_piece<COLS>(a, q, f, f1);
+            KvState<HD> st;
+            many_sweep<HD, NW>(a, q, p.h, p.c, p.t0, p.t1, sh, st);
+            const KvColumn col = kv_column(a, q, p.h, COLS * p.c + 32 * wave + lj);
+            const float l = st.l + __shfl_xor(st.l, 32);
+            if (col.mine) {
+                if (p.whole) {
+                    const float inv = kv_inverse(l);
+                    bf16* const to = a.o + (int64_t)col.row * a.o_row + (int64_t)col.head * a.o_head + 4 * lg;
+#pragma unroll
+                    for (int i = 0; i < DT * 4; ++i) {
+                        bf16x4 r;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) r[e] = (bf16)(st.o[i / 4][i % 4 * 4 + e] * inv);
+                        *(bf16x4*)(to + 8 * i) = r;
+                    }
+                } else {
+                    const int64_t at = (int64_t)(2 * w + p.from_start) * COLS + 32 * wave + lj;
+                    float* const to = a.part_o + at * HD + 4 * lg;
+#pragma unroll
+                    for (int i = 0; i < DT * 4; ++i)
+                        *(floatx4*)(to + 8 * i) = floatx4{st.o[i / 4][i % 4 * 4], st.o[i / 4][i % 4 * 4 + 1], st.o[i / 4][i % 4 * 4 + 2], st.o[i / 4][i % 4 * 4 + 3]};
+                    if (lg == 0) *(float2*)(a.part_ml + at * 2) = make_float2(st.mc, l);
+                }
+            }
+            __syncthreads();                           // the next piece's tiles go where this one's were
+            f = p.next;
+        }
+    }
+}
+
+// Joins the pieces of the column tiles that have several, in order: a workgroup per 32 columns, a lane per four dims of one.
+template <int HD, int COLS>
+__global__ __launch_bounds__(256) void kv_join_kernel(AttendArgs a, int most, int least) {
+    const int lane = threadIdx.x & 63;
+    const KvShares shares(kv_total<COLS>(a), most, least);
+    if (shares.total == 0) return;
+    // the column tile: sequences in order, then heads
     int64_t before = 0;
-    KvSeq q = {};
-    int unit = -1;
+    int passed = 0;                                            // column tiles of the sequences before base
     for (int base = 0; base < a.c.n_seqs; base += 64) {
-        const KvScan<32> s(a, base);
-        const int lane = threadIdx.x & 63;
-        int units = s.col_tiles(a) * a.c.heads;
+        const KvScan<COLS> s(a, base);
+        int units = s.s.ct * a.c.heads;
+#pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
             const int x = __shfl_up(units, o);
             units += lane >= o ? x : 0;
         }
-        const int want = (int)blockIdx.x - unit - 1;           // unit + 1: column tiles of the sequences before base
+        const int want = (int)blockIdx.x - passed;
         const uint64_t m = __ballot(want < units);
-        if (m) {
-            const int l = __builtin_ctzll(m);
-            q = s.pick(a, base, before, l);
-            unit = want - (__builtin_amdgcn_readlane(units, l) - q.ct * a.c.heads);
-            goto found;
+        if (!m) {
+            passed += __builtin_amdgcn_readlane(units, 63);
+            before += s.all();
+            continue;
         }
-        unit += __builtin_amdgcn_readlane(units, 63);
-        before += s.all();
-    }
-    return;
-found:
-    const int64_t f0 = q.first + (int64_t)unit * q.tiles;
-    const int w0 = parts.of(f0), w1 = parts.of(f0 + q.tiles - 1);
-    if (w0 == w1) return;
-    const int h = unit / q.ct, c = unit % q.ct, cols = min(32, q.n * a.times - 32 * c);
-    const int first = 2 * w0 + 1;
-    for (int i = threadIdx.x; i < cols * (HD / 4); i += 256) {
-        const int lj = i / (HD / 4), d = i % (HD / 4) * 4;
-        float m = kNoRef, sum = 0.0f;
-        for (int w = w0; w <= w1; ++w) m = fmaxf(m, a.part_ml[((int64_t)(w == w0 ? first : 2 * w) * 32 + lj) * 2]);
-        floatx4 v = {0.f, 0.f, 0.f, 0.f};
-        for (int w = w0; w <= w1; ++w) {
-            const int64_t at = (int64_t)(w == w0 ? first : 2 * w) * 32 + lj;
-            const float2 ml = *(const float2*)(a.part_ml + at * 2);
-            const float k = __builtin_amdgcn_exp2f(ml.x - m);
-            sum = fmaf(ml.y, k, sum);
-            const floatx4 p = *(const floatx4*)(a.part_o + at * HD + d);
+        const int l = __builtin_ctzll(m);
+        const KvSeq q = s.pick(a, base, before, l);
+        const int unit = want - (__builtin_amdgcn_readlane(units, l) - q.ct * a.c.heads), h = unit / q.ct, c = unit % q.ct;
+        const int64_t f0 = q.first + h * q.head() + q.before(c);
+        const int w0 = shares.of(f0), w1 = shares.of(f0 + q.w0 + (int64_t)c * q.dw - 1);
+        if (w0 == w1) return;
+        const int c0 = blockIdx.y * 32, cols = min(32, q.n * a.times - COLS * c - c0);
+        for (int i = threadIdx.x; i < cols * (HD / 4); i += 256) {
+            const int lj = i / (HD / 4), d = i % (HD / 4) * 4;
+            auto slot = [&](int w) { return (int64_t)(w == w0 ? 2 * w + 1 : 2 * w) * COLS + c0 + lj; };
+            float mx = kNoRef, sum = 0.0f;
+            for (int w = w0; w <= w1; ++w) mx = fmaxf(mx, a.part_ml[slot(w) * 2]);
+            floatx4 v = {0.f, 0.f, 0.f, 0.f};
+            for (int w = w0; w <= w1; ++w) {
+                const float2 ml = *(const float2*)(a.part_ml + slot(w) * 2);
+                const float k = __builtin_amdgcn_exp2f(ml.x - mx);
+                sum = fmaf(ml.y, k, sum);
+                const floatx4 p = *(const floatx4*)(a.part_o + slot(w) * HD + d);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = fmaf(p[e], k, v[e]);
+                for (int e = 0; e < 4; ++e) v[e] = fmaf(p[e], k, v[e]);
+            }
+            const float inv = kv_inverse(sum);
+            const KvColumn col = kv_column(a, q, h, COLS * c + c0 + lj);
+            bf16x4 r;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[e] = (bf16)(v[e] * inv);
+            *(bf16x4*)(a.o + (int64_t)col.row * a.o_row + (int64_t)col.head * a.o_head + d) = r;
         }
-        const float inv = kv_inverse(sum);
-        const KvColumn col = kv_column(a, q, h, 32 * c + lj);
-        bf16x4 r;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) r[e] = (bf16)(v[e] * inv);
-        *(bf16x4*)(a.o + (int64_t)col.row * a.o_row + (int64_t)col.head * a.o_head + d) = r;
+        return;
     }
 }
 
@@ -361,22 +552,39 @@ const char* query_bad(const cf_kv_cache* c, const cf_kv_query* x) {
     return nullptr;
 }
 
-constexpr int FEW_WGS = 512;           // two on each CU
+constexpr int FEW_WGS = 512, MANY_WGS = 256;           // two workgroups on each CU, one
 
 struct AttendPlan {
+    bool many;                         // kernel with MANY_WAVES * 32 columns per workgroup
+    int cols, wgs, least;
     int64_t units;                     // column tiles of all sequences and key heads, at most
-    uint64_t slots;                    // partial results of 32 columns
     uint64_t ml_offset, bytes;         // of the workspace
 };
+constexpr int MANY_WAVES = 8;
 const char* attend_plan(const cf_kv_cache* c, const cf_kv_query* x, AttendPlan* p) {
-    const int64_t times = x->heads / c->heads, cols = (int64_t)x->n_tokens * times;
-    if (cols > 0x7fffffff - 4096) return "too many queries";
-    p->units = (cols / 32 + std::min(c->n_seqs, x->n_tokens)) * c->heads;
+    const int64_t times = x->heads / c->heads, all = (int64_t)x->n_tokens * times, most = (x->max_q && x->max_q < x->n_tokens ? x->max_q : x->n_tokens) * times;
+    if (all > 0x7fffffff - 4096) return "too many queries";
+    p->many = most > 32;
+    p->cols = p->many ? 32 * MANY_WAVES : 32;
+    p->wgs = p->many ? MANY_WGS : FEW_WGS;
+    p->least = p->many ? MANY_LEAST : FEW_LEAST;
+    p->units = (all / p->cols + std::min(c->n_seqs, x->n_tokens)) * c->heads;
     if (p->units > 0x7fffffff) return "too many queries";
-    p->slots = 2 * FEW_WGS;
-    p->ml_offset = p->slots * 32 * c->head_dim * 4;
-    p->bytes = p->ml_offset + p->slots * 32 * 2 * 4;
+    const uint64_t slots = 2ull * p->wgs * p->cols;
+    p->ml_offset = slots * c->head_dim * 4;
+    p->bytes = p->ml_offset + slots * 2 * 4;
     return nullptr;
+}
+
+template <int HD>
+void launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
+    if (p.many) {
+        hipLaunchKernelGGL((kv_attend_many_kernel<HD, MANY_WAVES>), dim3(p.wgs), dim3(64 * MANY_WAVES), 0, s, a);
+        hipLaunchKernelGGL((kv_join_kernel<HD, 32 * MANY_WAVES>), dim3((unsigned)p.units, MANY_WAVES), dim3(256), 0, s, a, p.wgs, p.least);
+    } else {
+        hipLaunchKernelGGL(kv_attend_few_kernel<HD>, dim3(p.wgs), dim3(64 * FEW_WAVES), 0, s, a);
+        hipLaunchKernelGGL((kv_join_kernel<HD, 32>), dim3((unsigned)p.units), dim3(256), 0, s, a, p.wgs, p.least);
+    }
 }
 
 }  // namespace
@@ -416,13 +624,8 @@ extern "C" int cf_kv_attention(const cf_kv_cache* cache, const cf_kv_query* x, v
     a.part_o = (float*)workspace;
     a.part_ml = (float*)((char*)workspace + p.ml_offset);
     hipStream_t s = (hipStream_t)stream;
-    if (cache->head_dim == 128) {
-        hipLaunchKernelGGL(kv_attend_few_kernel<128>, dim3(FEW_WGS), dim3(64 * FEW_WAVES), 0, s, a);
-        hipLaunchKernelGGL(kv_join_kernel<128>, dim3((unsigned)p.units), dim3(256), 0, s, a, FEW_WGS);
-    } else {
-        hipLaunchKernelGGL(kv_attend_few_kernel<64>, dim3(FEW_WGS), dim3(64 * FEW_WAVES), 0, s, a);
-        hipLaunchKernelGGL(kv_join_kernel<64>, dim3((unsigned)p.units), dim3(256), 0, s, a, FEW_WGS);
-    }
+    if (cache->head_dim == 128) launch<128>(a, p, s);
+    else launch<64>(a, p, s);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? CF_OK : cf_fail(nullptr, CF_ERR_HIP, "kv_attention launch: %s", hipGetErrorString(e));
 }

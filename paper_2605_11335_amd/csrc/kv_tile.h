@@ -30,34 +30,45 @@ struct AttendArgs {
 
 constexpr int KV_TILE = 64;                // keys
 
-// A sequence of the batch, its column tiles and key tiles.  `first`: where its tiles begin when all (sequence, key head, column tile)s' key
-// tiles are laid end to end.
+// Work is laid end to end -- sequences, in each the key heads, in each the column tiles of COLS columns -- and cut into equal shares wherever that is.
+// The weight of a column tile is about the number of keys that it goes through: w0 + c dw for the c-th of a sequence (dw = 0 unless causal).
 struct KvSeq {
-    int b, start, n, len, ct, tiles;
-    int64_t first;
+    int b, start, n, len, ct;              // ct: column tiles
+    int w0, dw;
+    int64_t first;                         // where its work begins
+    __device__ __forceinline__ int64_t before(int c) const { return (int64_t)c * w0 + (int64_t)dw * ((int64_t)c * (c - 1) / 2); }        // of a head's column tiles before c
+    __device__ __forceinline__ int64_t head() const { return before(ct); }
 };
 
 // values that all lanes agree on, in scalar registers
 __device__ __forceinline__ int64_t kv_lane64(int64_t x, int lane) {
     return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, lane));
 }
-// The sequence of each lane, i = base + lane, and the inclusive sum of the key tiles up to it.
+template <int COLS>
+__device__ __forceinline__ void kv_weigh(const AttendArgs& a, KvSeq& s) {
+    s.ct = (s.n * a.times + COLS - 1) / COLS;
+    s.w0 = max(KV_TILE, s.len);            // (columns that see nothing have to be set to zero)
+    s.dw = 0;
+    if (a.causal && s.ct > 1) {
+        s.dw = COLS / a.times;             // query rows from one column tile to the next
+        s.w0 = max(KV_TILE, s.len - s.n + s.dw);
+    }
+}
+// The sequence of each lane, i = base + lane, and the inclusive sum of the work up to it.
 template <int COLS>
 struct KvScan {
-    int start, n, len;
+    KvSeq s;
     int64_t upto;
-    __device__ __forceinline__ int col_tiles(const AttendArgs& a) const { return (n * a.times + COLS - 1) / COLS; }
-    // an empty sequence has a tile, too, whose columns have to be set to zero
-    __device__ __forceinline__ static int key_tiles(int len) { return max(1, (len + KV_TILE - 1) / KV_TILE); }
     __device__ __forceinline__ KvScan(const AttendArgs& a, int base) {
         const int lane = threadIdx.x & 63, i = base + lane;
-        start = n = len = 0;
+        s.start = s.n = s.len = 0;
         if (i < a.c.n_seqs) {
-            start = kv_clamped(a.cu[i], 0, a.n_tokens);
-            n = kv_clamped(a.cu[i + 1], start, a.n_tokens) - start;
-            len = kv_clamped(a.lens[i], 0, a.c.capacity);
+            s.start = kv_clamped(a.cu[i], 0, a.n_tokens);
+            s.n = kv_clamped(a.cu[i + 1], s.start, a.n_tokens) - s.start;
+            s.len = kv_clamped(a.lens[i], 0, a.c.capacity);
         }
-        upto = (int64_t)col_tiles(a) * a.c.heads * key_tiles(len);
+        kv_weigh<COLS>(a, s);
+        upto = s.head() * a.c.heads;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
             const int64_t x = __shfl_up((long long)upto, o);
@@ -66,15 +77,14 @@ struct KvScan {
     }
     __device__ __forceinline__ int64_t all() const { return kv_lane64(upto, 63); }
     __device__ __forceinline__ KvSeq pick(const AttendArgs& a, int base, int64_t before, int lane) const {
-        KvSeq s;
-        s.b = base + lane;
-        s.start = __builtin_amdgcn_readlane(start, lane);
-        s.n = __builtin_amdgcn_readlane(n, lane);
-        s.len = __builtin_amdgcn_readlane(len, lane);
-        s.ct = (s.n * a.times + COLS - 1) / COLS;
-        s.tiles = key_tiles(s.len);
-        s.first = before + kv_lane64(upto, lane) - (int64_t)s.ct * a.c.heads * s.tiles;
-        return s;
+        KvSeq r;
+        r.b = base + lane;
+        r.start = __builtin_amdgcn_readlane(s.start, lane);
+        r.n = __builtin_amdgcn_readlane(s.n, lane);
+        r.len = __builtin_amdgcn_readlane(s.len, lane);
+        kv_weigh<COLS>(a, r);
+        r.first = before + kv_lane64(upto, lane) - r.head() * a.c.heads;
+        return r;
     }
 };
 template <int COLS>
@@ -83,7 +93,7 @@ __device__ __forceinline__ int64_t kv_total(const AttendArgs& a) {
     for (int base = 0; base < a.c.n_seqs; base += 64) t += KvScan<COLS>(a, base).all();
     return t;
 }
-// The sequence with tile f, 0 <= f < kv_total.
+// The sequence with work f, 0 <= f < kv_total.
 template <int COLS>
 __device__ __forceinline__ KvSeq kv_find(const AttendArgs& a, int64_t f) {
     int64_t before = 0;
@@ -94,6 +104,58 @@ __device__ __forceinline__ KvSeq kv_find(const AttendArgs& a, int64_t f) {
         before += s.all();
     }
 }
+
+// A column tile and a share of its keys: tiles [t0, t1) of `tiles`.
+struct KvPiece {
+    int h, c, t0, t1;
+    bool from_start, whole;
+    int64_t next;                          // where the work after it begins
+};
+// The piece of sequence s that begins at f, in a share that ends at f1.
+template <int COLS>
+__device__ __forceinline__ KvPiece kv_piece(const AttendArgs& a, const KvSeq& s, int64_t f, int64_t f1) {
+    KvPiece p;
+    const int64_t per = s.head();
+    int64_t x = f - s.first;
+    p.h = (int)(x / per);
+    x -= p.h * per;
+    int lo = 0, hi = s.ct - 1;             // the last column tile that begins at or before x
+    if (s.dw == 0) {
+        lo = (int)(x / s.w0);
+    } else {
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (s.before(mid) <= x) lo = mid;
+            else hi = mid - 1;
+        }
+    }
+    p.c = lo;
+    x -= s.before(p.c);
+    const int64_t w = s.w0 + (int64_t)p.c * s.dw, to = min(w, x + (f1 - f));
+    const int cols = min(COLS, s.n * a.times - COLS * p.c);
+    const int last = (COLS * p.c + cols - 1) / a.times;
+    const int end = a.causal ? min(s.len, s.len - s.n + last + 1) : s.len;           // of the keys that any column sees
+    const int tiles = (max(end, 0) + KV_TILE - 1) / KV_TILE;
+    p.t0 = (int)(x * tiles / w);
+    p.t1 = (int)(to * tiles / w);
+    p.from_start = x == 0;
+    p.whole = x == 0 && to == w;
+    p.next = f + (to - x);
+    return p;
+}
+// Equal shares of all work for up to `most` workgroups, none of less than `least`.
+struct KvShares {
+    int64_t total;
+    int wgs;
+    __device__ __forceinline__ KvShares(int64_t all, int most, int least) : total(all), wgs((int)max((int64_t)1, min((int64_t)most, (all + least - 1) / least))) {}
+    __device__ __forceinline__ int64_t begin(int w) const { return total * w / wgs; }
+    __device__ __forceinline__ int of(int64_t f) const {           // the workgroup with work f
+        int w = (int)(f * wgs / total);
+        while (begin(w + 1) <= f) ++w;
+        while (begin(w) > f) --w;
+        return w;
+    }
+};
 
 // A lane's column of a column tile.
 struct KvColumn {
@@ -165,12 +227,14 @@ __device__ __forceinline__ void kv_softmax(KvState<HD>& st, const floatx16 (&s)[
         psum = (ps[0] + ps[1]) + (ps[2] + ps[3]);
     };
     weigh();
-    if (__any(!(psum < 1048576.0f))) {
+    const bool over = !(psum < 1048576.0f);
+    if (__any(over)) {                     // (only the columns that need it move: a column's bits do not depend on those beside it)
         float mx = s[0][0];
 #pragma unroll
         for (int v = 1; v < 32; ++v) mx = fmaxf(mx, s[v >> 4][v & 15]);
         mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float mc = fmaxf(st.mc, mx * c2), f = __builtin_amdgcn_exp2f(st.mc - mc);
+        const int other = __shfl_xor((int)over, 32);
+        const float mc = over || other ? fmaxf(st.mc, mx * c2) : st.mc, f = __builtin_amdgcn_exp2f(st.mc - mc);
         st.mc = mc;
         st.l *= f;
 #pragma unroll
