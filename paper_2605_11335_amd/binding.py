@@ -524,36 +524,46 @@ def _refuse(cond, msg: str) -> None:
         raise ChunkflowError(CF_ERR_ARG, msg)
 
 
+# (Small calls take about as long as what is done here for them: nothing is formatted before it is known to be needed.)
 def _dtype_of(t) -> int:
-    if not _TYPES:
+    code = _TYPES.get(t.dtype)
+    if code is None:
         import torch
         _TYPES.update({torch.bfloat16: CF_BF16, torch.float32: CF_F32})
-    code = _TYPES.get(t.dtype)
-    _refuse(code is None, f"{t.dtype} is neither bfloat16 nor float32")
+        code = _TYPES.get(t.dtype)
+        if code is None:
+            raise ChunkflowError(CF_ERR_ARG, f"{t.dtype} is neither bfloat16 nor float32")
     return code
 
 
 def _launch(fn, name: str, device, stream, *args) -> None:
     """fn(*args, stream) on `device`, which has to be a GPU."""
     import torch
-    _refuse(device.type != "cuda", f"{name}: tensors on {device}, not on a GPU")
+    if device.type != "cuda":
+        raise ChunkflowError(CF_ERR_ARG, f"{name}: tensors on {device}, not on a GPU")
+    cuda, index = torch.cuda, device.index
     if stream is None:
-        stream = torch.cuda.current_stream(device)
-    _refuse(stream.device != device, f"{name}: a stream of {stream.device} for tensors on {device}")
-    if torch.cuda.current_device() == device.index:
-        _check(fn(*args, stream.cuda_stream))
+        stream = cuda.current_stream(index)
+    elif stream.device_index != index:
+        raise ChunkflowError(CF_ERR_ARG, f"{name}: a stream of GPU {stream.device_index} for tensors on {device}")
+    if cuda.current_device() == index:
+        rc = fn(*args, stream.cuda_stream)
     else:
-        with torch.cuda.device(device):
-            _check(fn(*args, stream.cuda_stream))
+        with cuda.device(index):
+            rc = fn(*args, stream.cuda_stream)
+    if rc != 0:
+        _check(rc)
 
 
-def _dense(t, what: str, dtypes, shape, device=None) -> int:
-    """The pointer of a dense tensor of that shape and one of those types on `device`."""
-    _refuse(t.dtype not in dtypes, f"{what}: {t.dtype}, expected {' or '.join(str(d) for d in dtypes)}")
-    _refuse(tuple(t.shape) != tuple(shape), f"{what}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    _refuse(not t.is_contiguous(), f"{what} is not dense")
-    _refuse(device is not None and t.device != device, f"{what} is on {t.device}, other tensors on {device}")
-    return t.data_ptr()
+def _dense(t, what: str, dtype, shape: tuple, device=None) -> int:
+    """The pointer of a dense tensor of that shape and type (or one of those) on `device`."""
+    if (t.dtype == dtype or (type(dtype) is tuple and t.dtype in dtype)) and t.shape == shape and t.is_contiguous() and (device is None or t.device == device):
+        return t.data_ptr()
+    if t.dtype != dtype and not (type(dtype) is tuple and t.dtype in dtype):
+        raise ChunkflowError(CF_ERR_ARG, f"{what}: {t.dtype}, expected {dtype}")
+    if t.shape != shape:
+        raise ChunkflowError(CF_ERR_ARG, f"{what}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    raise ChunkflowError(CF_ERR_ARG, f"{what} is not dense" if not t.is_contiguous() else f"{what} is on {t.device}, other tensors on {device}")
 
 
 def cf_rope_plan(head_dim: int, axis_pairs, theta=10000.0) -> cf_rope:
@@ -570,9 +580,9 @@ def cf_rope_tables(rope: cf_rope, pos, cos_out, sin_out, stream=None) -> None:
     """cos_out, sin_out [n, head_dim / 2] float32 of pos [n, axes] int32: what cf_block_io takes as rope_cos and rope_sin."""
     import torch
     n = pos.shape[0]
-    p = _dense(pos, "rope_tables: pos", (torch.int32,), (n, rope.n_axes))
-    c = _dense(cos_out, "rope_tables: cos_out", (torch.float32,), (n, rope.head_dim // 2), pos.device)
-    s = _dense(sin_out, "rope_tables: sin_out", (torch.float32,), (n, rope.head_dim // 2), pos.device)
+    p = _dense(pos, "rope_tables: pos", torch.int32, (n, rope.n_axes))
+    c = _dense(cos_out, "rope_tables: cos_out", torch.float32, (n, rope.head_dim // 2), pos.device)
+    s = _dense(sin_out, "rope_tables: sin_out", torch.float32, (n, rope.head_dim // 2), pos.device)
     _launch(lib().cf_rope_tables, "rope_tables", pos.device, stream, C.byref(rope), p, n, c, s)
 
 
@@ -583,11 +593,16 @@ def _strides(t) -> tuple:
 
 
 def _rope_operand(rope, x, y, n, like, which) -> tuple:
-    _refuse(x.dim() != 3 or x.shape[0] != n or x.shape[2] != rope.head_dim, f"rope_apply: {which} has shape {tuple(x.shape)}, expected ({n}, heads, {rope.head_dim})")
-    _refuse(y.shape != x.shape, f"rope_apply: {which} and its output differ in shape")
-    _refuse(x.dtype != like.dtype or y.dtype != like.dtype, f"rope_apply: {which}: one type for all operands")
-    _refuse(x.stride(2) != 1 or y.stride(2) != 1, f"rope_apply: {which}: the last dimension is not dense")
-    _refuse(x.device != like.device or y.device != like.device, f"rope_apply: {which}: operands on several devices")
+    if x.dim() != 3 or x.shape[0] != n or x.shape[2] != rope.head_dim:
+        raise ChunkflowError(CF_ERR_ARG, f"rope_apply: {which} has shape {tuple(x.shape)}, expected ({n}, heads, {rope.head_dim})")
+    if y.shape != x.shape:
+        raise ChunkflowError(CF_ERR_ARG, f"rope_apply: {which} and its output differ in shape")
+    if x.dtype != like.dtype or y.dtype != like.dtype:
+        raise ChunkflowError(CF_ERR_ARG, f"rope_apply: {which}: one type for all operands")
+    if x.stride(2) != 1 or y.stride(2) != 1:
+        raise ChunkflowError(CF_ERR_ARG, f"rope_apply: {which}: the last dimension is not dense")
+    if x.device != like.device or y.device != like.device:
+        raise ChunkflowError(CF_ERR_ARG, f"rope_apply: {which}: operands on several devices")
     return x.data_ptr(), y.data_ptr(), *_strides(x), *_strides(y), x.shape[1], 0
 
 
@@ -596,7 +611,7 @@ def cf_rope_apply(rope: cf_rope, pos, q, q_out, k=None, k_out=None, inverse: boo
     where the output is the input."""
     import torch
     n = q.shape[0]
-    p = _dense(pos, "rope_apply: pos", (torch.int32,), (n, rope.n_axes), q.device)
+    p = _dense(pos, "rope_apply: pos", torch.int32, (n, rope.n_axes), q.device)
     _refuse((k is None) != (k_out is None), "rope_apply: k and k_out go together")
     ops = (cf_rope_operand * 2)()
     ops[0] = _rope_operand(rope, q, q_out, n, q, "q")
@@ -618,8 +633,8 @@ class KVCache:
         self.device, self.head_dim, self.heads, self.n_seqs = k.device, chunks * 16, heads, table.shape[0]
         self.tensors = (k, v, scales, table)
         self.c = cf_kv_cache(_dense(k, "kv_cache: k", codes, k.shape), _dense(v, "kv_cache: v", codes, (pages, heads, groups, chunks * 16, 16), k.device),
-                             _dense(scales, "kv_cache: scales", (torch.uint8,), (pages, heads, groups, 2), k.device),
-                             _dense(table, "kv_cache: table", (torch.int32,), table.shape, k.device),
+                             _dense(scales, "kv_cache: scales", torch.uint8, (pages, heads, groups, 2), k.device),
+                             _dense(table, "kv_cache: table", torch.int32, table.shape, k.device),
                              pages, groups * 16, heads, chunks * 16, table.shape[0], table.shape[1])
         self.ref = C.byref(self.c)
 
@@ -631,21 +646,23 @@ def make_kv_cache(k, v, scales, table) -> KVCache:
 
 
 def _batch(cache, what: str, cu, lens) -> tuple:
+    """Pointers of offsets [sequences + 1] and lengths [sequences]."""
     import torch
-    return _dense(cu, what + ": cu", (torch.int32,), (cache.n_seqs + 1,), cache.device), _dense(lens, what + ": lens", (torch.int32,), (cache.n_seqs,), cache.device)
+    return _dense(cu, what, torch.int32, (cache.n_seqs + 1,), cache.device), _dense(lens, what, torch.int32, (cache.n_seqs,), cache.device)
 
 
 def cf_kv_append(cache: KVCache, k, v, cu, lens, rope: Optional[cf_rope] = None, pos=None, stream=None) -> None:
     """Rows cu[b] .. cu[b+1] of k and v [tokens, heads, head_dim] (bf16 or fp32) become tokens lens[b], ... of sequence b, k turned by pos if a plan is given."""
     import torch
     n, want = k.shape[0], (cache.heads, cache.head_dim)
-    _refuse(k.dim() != 3 or k.shape[1:] != want or v.shape != k.shape, f"kv_append: k {tuple(k.shape)} and v {tuple(v.shape)}, expected [tokens, {want[0]}, {want[1]}]")
+    if k.dim() != 3 or k.shape[1:] != want or v.shape != k.shape:
+        raise ChunkflowError(CF_ERR_ARG, f"kv_append: k {tuple(k.shape)} and v {tuple(v.shape)}, expected [tokens, {want[0]}, {want[1]}]")
     _refuse(v.dtype != k.dtype, "kv_append: k and v differ in type")
     _refuse(k.stride(2) != 1 or v.stride(2) != 1, "kv_append: the last dimension is not dense")
     _refuse(k.device != cache.device or v.device != cache.device, "kv_append: tensors on several devices")
     _refuse((rope is None) != (pos is None), "kv_append: a plan and positions go together")
-    at = None if rope is None else _dense(pos, "kv_append: pos", (torch.int32,), (n, rope.n_axes), cache.device)
-    x = cf_kv_new(k.data_ptr(), v.data_ptr(), *_strides(k), *_strides(v), *_batch(cache, "kv_append", cu, lens),
+    at = None if rope is None else _dense(pos, "kv_append: pos", torch.int32, (n, rope.n_axes), cache.device)
+    x = cf_kv_new(k.data_ptr(), v.data_ptr(), *_strides(k), *_strides(v), *_batch(cache, "kv_append: cu, lens", cu, lens),
                   None if rope is None else C.pointer(rope), at, n, _dtype_of(k))
     _launch(lib().cf_kv_append, "kv_append", cache.device, stream, cache.ref, C.byref(x))
 
@@ -663,12 +680,13 @@ def cf_kv_attention(cache: KVCache, q, o, cu, lens, causal: bool = False, scale:
     if not given.  workspace: a dense tensor of cf_kv_attention_workspace bytes."""
     import torch
     n = q.shape[0]
-    _refuse(q.dim() != 3 or q.shape[2] != cache.head_dim or o.shape != q.shape, f"kv_attention: q {tuple(q.shape)} and o {tuple(o.shape)}, expected [tokens, heads, {cache.head_dim}]")
+    if q.dim() != 3 or q.shape[2] != cache.head_dim or o.shape != q.shape:
+        raise ChunkflowError(CF_ERR_ARG, f"kv_attention: q {tuple(q.shape)} and o {tuple(o.shape)}, expected [tokens, heads, {cache.head_dim}]")
     _refuse(q.dtype != torch.bfloat16 or o.dtype != torch.bfloat16, "kv_attention: q and o must be bfloat16")
     _refuse(q.stride(2) != 1 or o.stride(2) != 1, "kv_attention: the last dimension is not dense")
     _refuse(q.device != cache.device or o.device != cache.device or (workspace is not None and workspace.device != cache.device), "kv_attention: tensors on several devices")
     _refuse(workspace is not None and not workspace.is_contiguous(), "kv_attention: the workspace is not dense")
-    x = cf_kv_query(q.data_ptr(), o.data_ptr(), *_strides(q), *_strides(o), *_batch(cache, "kv_attention", cu, lens), n, q.shape[1], max_q, int(causal),
+    x = cf_kv_query(q.data_ptr(), o.data_ptr(), *_strides(q), *_strides(o), *_batch(cache, "kv_attention: cu, lens", cu, lens), n, q.shape[1], max_q, int(causal),
                     cache.head_dim ** -0.5 if scale is None else scale, 0)
     _launch(lib().cf_kv_attention, "kv_attention", cache.device, stream, cache.ref, C.byref(x), _ptr(workspace),
             0 if workspace is None else workspace.numel() * workspace.element_size())

@@ -280,31 +280,39 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attend_few_kernel(Attend
 // Many columns: a workgroup of NW waves has 32 NW columns of a (sequence, key head) and goes through its share of the keys, tiles of 64 that all its
 // waves use.  Bound by the matrix cores and, nearly as much, by reading fragments from LDS.  Codes become bf16 once per workgroup, on their way into
 // LDS: a lane's 16 bytes are two fragments' worth (kv_tile.h), stored as the fragments lie, so that a fragment read is 1 KiB in order and
-// nothing has to be swizzled.  Tile t + 2 is on its way from memory and t + 1 is converted into the other buffer while t is computed.
+// nothing has to be swizzled.  Page t + 3, codes of t + 2 are on their way from memory and t + 1 is converted into the other buffer while tile t is computed.
 struct ManyFlags {
     uint32_t held;                                     // tokens of each of the tile's groups, a byte each
-    uint32_t nan;                                      // t + 1 where a value of tile t was NaN and not every column sees the tile whole
+    uint32_t nan;                                      // t + 1 where a value of tile t was NaN
 };
-template <int HD, int NW>
+template <int HD>
 struct ManyShared {
     bf16x8 k[2][2][HD / 16][64], v[2][4][HD / 32][64];
-    uint16_t nan_of[2][4 * HD];                        // which of a V chunk's 16 tokens were NaN, in such a tile
+    // of tiles that not every column sees whole:
+    uint16_t nan_of[2][4 * HD];                        // which of a V chunk's 16 tokens were NaN
     ManyFlags flags[2];
 };
 
 template <int HD, int NW>
-__device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, int h, int c, int t0, int t1, ManyShared<HD, NW>& sh, KvState<HD>& st) {
+__device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, int h, int c, int t0, int t1, ManyShared<HD>& sh, KvState<HD>& st) {
     constexpr int KS = HD / 16, DT = HD / 32, NT = 64 * NW, GB = 16 * HD;
-    constexpr int CHUNKS = 4 * HD, PER = CHUNKS >= NT ? CHUNKS / NT : 1;        // 16-byte chunks of a tile's K; of those and of V, a lane has PER
+    constexpr int CHUNKS = 4 * HD, PER = CHUNKS >= NT ? CHUNKS / NT : 1;        // 16-byte chunks of a tile's K; of those and of V's, a lane has PER
     constexpr bool BOTH = CHUNKS >= NT;                                         // else half of the lanes have K, half V
     static_assert(CHUNKS % NT == 0 || 2 * CHUNKS == NT, "");
     const int tid = threadIdx.x, lane = tid & 63, lj = lane & 31, lg = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col0 = 32 * NW * c + 32 * wave, cols = min(32, q.n * a.times - col0);            // (cols <= 0: a wave without a column only copies)
     const KvColumn col = kv_column(a, q, h, col0 + lj);
-    const int end_least = cols > 0 ? __builtin_amdgcn_readlane(col.end, 0) : 0x7fffffff, end_most = cols > 0 ? __builtin_amdgcn_readlane(col.end, cols - 1) : 0;
-    const int wg_least = a.causal ? min(q.len, q.len - q.n + 32 * NW * c / a.times + 1) : q.len;             // of all waves
     st.clear();
     if (t0 >= t1) return;
+    const int32_t* const table = a.c.table + (int64_t)q.b * a.c.table_stride;
+    // tiles [t0, t_plain) are seen whole by every column of the workgroup and have all their pages
+    const int least = a.causal ? min(q.len, q.len - q.n + 32 * NW * c / a.times + 1) : q.len;
+    int t_plain = max(t0, min(t1, max(least, 0) / KV_TILE));
+    {
+        bool hole = false;
+        for (int p = (t0 * KV_TILE >> a.c.page_shift) + tid; p <= (t_plain * KV_TILE - 1) >> a.c.page_shift; p += NT) hole |= (uint32_t)table[p] >= (uint32_t)a.c.n_pages;
+        if (__syncthreads_or(hole)) t_plain = t0;
+    }
     bf16x8 qf[KS];
     {
         const bf16* const p = a.q + (int64_t)col.row * a.q_row + (int64_t)col.head * a.q_head + 16 * lg;
@@ -314,43 +322,59 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
     // ---- copies.  Chunk x of K or V: group x / HD of the tile, 16 bytes x % HD of it.
     const bool has_k = BOTH || tid < CHUNKS, has_v = BOTH || tid >= CHUNKS;
     const int x0 = BOTH ? tid : tid % CHUNKS;
-    int g_of[PER];                                     // groups of the tile that is looked up
+    const int last = q.len - 1, page_mask = (1 << a.c.page_shift) - 1;
+    int page[PER];                                     // of the tile after the one in flight
     uint32_t pw[PER];                                  // powers of the one in flight
-    uint32_t held[PER];                                // its tokens there are
+    int held[PER];                                     // how many tokens of its groups there are
     uint32x4 kr[PER], vr[PER];
-    auto look_up = [&](int t) __attribute__((always_inline)) {
+    auto look_up = [&](int t) __attribute__((always_inline)) {          // (past the end: some page of the sequence's)
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int64_t p = (int64_t)t * KV_TILE + 16 * ((i * NT + x0) / HD);
-            g_of[i] = t < t1 && p < q.len ? kv_group(a.c, q.b, h, (int)p) : -1;
-        }
+        for (int i = 0; i < PER; ++i) page[i] = table[min(t * KV_TILE + 16 * ((i * NT + x0) / HD), last) >> a.c.page_shift];
     };
     auto fetch = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int x = i * NT + x0, g = max(g_of[i], 0);
-            held[i] = g_of[i] < 0 ? 0 : min(max(q.len - (t * KV_TILE + 16 * (x / HD)), 0), 16);
+            const int x = i * NT + x0, p = t * KV_TILE + 16 * (x / HD);
+            const bool there = (uint32_t)page[i] < (uint32_t)a.c.n_pages;
+            held[i] = there ? min(max(q.len - p, 0), 16) : 0;
+            const int g = there ? ((page[i] * a.c.heads + h) << (a.c.page_shift - 4)) + ((p & page_mask) >> 4) : 0;
             pw[i] = *(const uint16_t*)(a.c.scales + 2 * (int64_t)g);
-            if (has_k) kr[i] = *(const uint32x4*)(a.c.k + (int64_t)g * GB + (x % HD) * 16);
-            if (has_v) vr[i] = *(const uint32x4*)(a.c.v + (int64_t)g * GB + (x % HD) * 16);
+            const uint32_t r = (x % HD) * 16;
+            if (has_k) kr[i] = *(const uint32x4*)(a.c.k + (int64_t)g * GB + r);
+            if (has_v) vr[i] = *(const uint32x4*)(a.c.v + (int64_t)g * GB + r);
         }
     };
     auto convert = [&](int t, int buf) __attribute__((always_inline)) {
-        const bool part = (t + 1) * KV_TILE > wg_least;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int x = i * NT + x0, grp = x / HD, r = x % HD;
             uint32_t pk = pw[i] & 255u, pv = pw[i] >> 8;
-            if (__any(held[i] < 16 || pk == 255u || pv == 255u)) {
+            if (t >= t_plain || __any(pk == 255u || pv == 255u)) {
                 const bool nk = pk == 255u, nv = pv == 255u;
                 pk = nk || held[i] == 0 ? 127u : pk;
                 pv = nv || held[i] == 0 ? 127u : pv;
+                uint32_t m = 0;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    const int b = min(max((int)held[i] - 4 * w, 0), 4);
+                    const int b = min(max(held[i] - 4 * w, 0), 4);
                     const uint32_t keep = b == 4 ? ~0u : (1u << (8 * b)) - 1u;
-                    kr[i][w] = nk ? 0x7f7f7f7fu : kr[i][w];
-                    vr[i][w] = (nv ? 0x7f7f7f7fu : vr[i][w]) & keep;
+                    if (has_k) kr[i][w] = nk ? 0x7f7f7f7fu : kr[i][w];
+                    if (has_v) {
+                        uint32_t v = (nv ? 0x7f7f7f7fu : vr[i][w]) & keep;
+                        if (t >= t_plain) {
+                            const uint32_t nans = kv_nan_codes(v);
+                            v = kv_without_nan(v, nans);
+                            m |= ((nans >> 7) * 0x10204080u >> 28) << (4 * w);      // four bits side by side
+                        }
+                        vr[i][w] = v;
+                    }
+                }
+                if (t >= t_plain) {
+                    if (has_v) {
+                        sh.nan_of[buf][x] = (uint16_t)m;
+                        if (m) sh.flags[buf].nan = (uint32_t)t + 1;
+                    }
+                    if (has_k && r == 0) ((uint8_t*)&sh.flags[buf].held)[grp] = (uint8_t)held[i];
                 }
             }
             if (has_k) {
@@ -360,62 +384,102 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
                 sh.k[buf][grp >> 1][ch | 1][to] = kv_wide(kr[i][2], kr[i][3], f);
             }
             if (has_v) {
-                if (part) {
-                    uint32_t m = 0;
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const uint32_t nans = kv_nan_codes(vr[i][w]);
-                        vr[i][w] = kv_without_nan(vr[i][w], nans);
-                        m |= ((nans >> 7) * 0x10204080u >> 28) << (4 * w);          // four bits side by side
-                    }
-                    sh.nan_of[buf][x] = (uint16_t)m;
-                    if (m) sh.flags[buf].nan = (uint32_t)t + 1;
-                }
                 const int to = (r & 31) + 32 * (grp & 1);
                 const float f = kv_power(pv);
                 sh.v[buf][grp & ~1][r >> 5][to] = kv_wide(vr[i][0], vr[i][1], f);
                 sh.v[buf][grp | 1][r >> 5][to] = kv_wide(vr[i][2], vr[i][3], f);
             }
-            if (has_k && r == 0) ((uint8_t*)&sh.flags[buf].held)[grp] = (uint8_t)held[i];
         }
+    };
+    // while a tile is computed: the next one into LDS, the one after on its way
+    auto copies = [&](int t, int buf) __attribute__((always_inline)) {
+        if (t + 1 < t1) convert(t + 1, buf ^ 1);
+        if (t + 2 < t1) {
+            fetch(t + 2);
+            look_up(t + 3);
+        }
+    };
+    floatx16 s[2];
+    bf16x8 pf[4];
+    // S^T = K Q^T: MFMA i has half i & 1 of the keys and k-step i >> 1; fragments run four reads ahead
+    auto scores = [&](int buf) __attribute__((always_inline)) {
+        bf16x8 kf[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kf[i] = sh.k[buf][i & 1][i >> 1][lane];
+#pragma unroll
+        for (int i = 0; i < 2 * KS; ++i) {
+            floatx16 z;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) z[v] = 0.0f;
+            s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i & 3], qf[i >> 1], i < 2 ? z : s[i & 1], 0, 0, 0);
+            if (i + 4 < 2 * KS) kf[i & 3] = sh.k[buf][i & 1][(i + 4) >> 1][lane];
+        }
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+        for (int i = 0; i < 2 * KS - 4; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+    };
+    // O^T += V^T P^T: MFMA i has k-step i / DT and dims 32 (i % DT) ...; the first fragments are read before the softmax
+    bf16x8 vf[4];
+    auto first_values = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) vf[i] = sh.v[buf][i / DT][i % DT][lane];
+    };
+    auto values = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4 * DT; ++i) {
+            st.o[i % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i & 3], pf[i / DT], st.o[i % DT], 0, 0, 0);
+            if (i + 4 < 4 * DT) vf[i & 3] = sh.v[buf][(i + 4) / DT][(i + 4) % DT][lane];
+        }
+#pragma unroll
+        for (int i = 0; i < 4 * DT - 4; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 1);
     };
     if (tid < 2) sh.flags[tid].nan = 0;
     look_up(t0);
     fetch(t0);
     look_up(t0 + 1);
-    __syncthreads();                                   // the flags are cleared; what the buffers held before has been read
+    __syncthreads();                                   // the flags are cleared (and what the buffers held before has been read)
     convert(t0, t0 & 1);
     fetch(t0 + 1);
     look_up(t0 + 2);
     __syncthreads();
-    for (int t = t0; t < t1; ++t) {
-        const int buf = t & 1;
-        if (t + 1 < t1) convert(t + 1, buf ^ 1);
-        if (t + 2 < t1) fetch(t + 2);
-        look_up(t + 3);
-        if (t * KV_TILE < end_most) {
-            const uint32_t there = sh.flags[buf].held;
-            const bool nan = sh.flags[buf].nan == (uint32_t)t + 1;
-            const bool part = __builtin_amdgcn_readfirstlane(there) != 0x10101010u || (t + 1) * KV_TILE > end_least;
-            floatx16 s[2];
-#pragma unroll
-            for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) s[mt][v] = 0.0f;
-#pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(sh.k[buf][0][k][lane], qf[k], s[0], 0, 0, 0);
-                s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(sh.k[buf][1][k][lane], qf[k], s[1], 0, 0, 0);
-            }
-            int rel[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) rel[i] = min((int)(there >> (8 * (2 * i + lg)) & 255u), min(max(col.end - (t * KV_TILE + 32 * i + 16 * lg), 0), 16));
-            if (part) kv_mask(s, rel);
+    int t = t0;
+    if (cols > 0) {
+        for (; t < t_plain; ++t) {
+            const int buf = t & 1;
+            copies(t, buf);
             __builtin_amdgcn_sched_barrier(0);
-            bf16x8 pf[4];
+            scores(buf);
+            first_values(buf);
+            __builtin_amdgcn_sched_barrier(0);
             kv_softmax<HD>(st, s, a.c2, pf);
             __builtin_amdgcn_sched_barrier(0);
-            if (__builtin_amdgcn_readfirstlane(nan)) {
+            values(buf);
+            __syncthreads();                           // tile t + 1 is in its buffer, that of t is free
+        }
+    }
+    const int end_most = cols > 0 ? __builtin_amdgcn_readlane(col.end, cols - 1) : 0;
+    for (; t < t1; ++t) {
+        const int buf = t & 1;
+        copies(t, buf);
+        if (t * KV_TILE < end_most) {
+            scores(buf);
+            int rel[2];
+            const uint32_t there = sh.flags[buf].held;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) rel[i] = min((int)(there >> (8 * (2 * i + lg)) & 255u), min(max(col.end - (t * KV_TILE + 32 * i + 16 * lg), 0), 16));
+            kv_mask(s, rel);
+            __builtin_amdgcn_sched_barrier(0);
+            kv_softmax<HD>(st, s, a.c2, pf);
+            __builtin_amdgcn_sched_barrier(0);
+            if (__builtin_amdgcn_readfirstlane(sh.flags[buf].nan) == (uint32_t)t + 1) {
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
                     floatx16 hits;
@@ -434,12 +498,10 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-                for (int d = 0; d < DT; ++d) st.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(sh.v[buf][ks][d][lane], pf[ks], st.o[d], 0, 0, 0);
+            first_values(buf);
+            values(buf);
         }
-        __syncthreads();                               // tile t + 1 is in its buffer, that of t is free
+        __syncthreads();
     }
 }
 
@@ -447,7 +509,7 @@ constexpr int MANY_LEAST = 8 * KV_TILE;                // keys that are worth a 
 template <int HD, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a) {
     constexpr int DT = HD / 32, COLS = 32 * NW;
-    __shared__ ManyShared<HD, NW> sh;
+    __shared__ ManyShared<HD> sh;
     const int lane = threadIdx.x & 63, lj = lane & 31, lg = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const KvShares shares(kv_total<COLS>(a), gridDim.x, MANY_LEAST);
     if ((int)blockIdx.x >= shares.wgs || shares.total == 0) return;
