@@ -2,6 +2,7 @@
 // sequence's length, of pages that the table does not name and, causal, behind the query take no part, whatever their codes are.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "context.h"
 #include "kv_tile.h"
@@ -344,7 +345,8 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
             if (has_v) vr[i] = *(const uint32x4*)(a.c.v + (int64_t)g * GB + r);
         }
     };
-    auto convert = [&](int t, int buf) __attribute__((always_inline)) {
+    auto convert = [&](int t, auto buf_c) __attribute__((always_inline)) {
+        constexpr int buf = decltype(buf_c)::value;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int x = i * NT + x0, grp = x / HD, r = x % HD;
@@ -392,8 +394,8 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
         }
     };
     // while a tile is computed: the next one into LDS, the one after on its way
-    auto copies = [&](int t, int buf) __attribute__((always_inline)) {
-        if (t + 1 < t1) convert(t + 1, buf ^ 1);
+    auto copies = [&](int t, auto buf_c) __attribute__((always_inline)) {
+        if (t + 1 < t1) convert(t + 1, std::integral_constant<int, 1 - decltype(buf_c)::value>{});
         if (t + 2 < t1) {
             fetch(t + 2);
             look_up(t + 3);
@@ -402,7 +404,8 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
     floatx16 s[2];
     bf16x8 pf[4];
     // S^T = K Q^T: MFMA i has half i & 1 of the keys and k-step i >> 1; fragments run four reads ahead
-    auto scores = [&](int buf) __attribute__((always_inline)) {
+    auto scores = [&](auto buf_c) __attribute__((always_inline)) {
+        constexpr int buf = decltype(buf_c)::value;
         bf16x8 kf[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) kf[i] = sh.k[buf][i & 1][i >> 1][lane];
@@ -424,11 +427,13 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
     };
     // O^T += V^T P^T: MFMA i has k-step i / DT and dims 32 (i % DT) ...; the first fragments are read before the softmax
     bf16x8 vf[4];
-    auto first_values = [&](int buf) __attribute__((always_inline)) {
+    auto first_values = [&](auto buf_c) __attribute__((always_inline)) {
+        constexpr int buf = decltype(buf_c)::value;
 #pragma unroll
         for (int i = 0; i < 4; ++i) vf[i] = sh.v[buf][i / DT][i % DT][lane];
     };
-    auto values = [&](int buf) __attribute__((always_inline)) {
+    auto values = [&](auto buf_c) __attribute__((always_inline)) {
+        constexpr int buf = decltype(buf_c)::value;
 #pragma unroll
         for (int i = 0; i < 4 * DT; ++i) {
             st.o[i % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i & 3], pf[i / DT], st.o[i % DT], 0, 0, 0);
@@ -446,33 +451,30 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
     fetch(t0);
     look_up(t0 + 1);
     __syncthreads();                                   // the flags are cleared (and what the buffers held before has been read)
-    convert(t0, t0 & 1);
+    convert(t0, std::integral_constant<int, 0>{});
     fetch(t0 + 1);
     look_up(t0 + 2);
     __syncthreads();
-    int t = t0;
-    if (cols > 0) {
-        for (; t < t_plain; ++t) {
-            const int buf = t & 1;
-            copies(t, buf);
-            __builtin_amdgcn_sched_barrier(0);
-            scores(buf);
-            first_values(buf);
-            __builtin_amdgcn_sched_barrier(0);
-            kv_softmax<HD>(st, s, a.c2, pf);
-            __builtin_amdgcn_sched_barrier(0);
-            values(buf);
-            __syncthreads();                           // tile t + 1 is in its buffer, that of t is free
-        }
-    }
+    // tile t is in buffer (t - t0) & 1
+    auto plain = [&](int t, auto buf_c) __attribute__((always_inline)) {
+        copies(t, buf_c);
+        __builtin_amdgcn_sched_barrier(0);
+        scores(buf_c);
+        first_values(buf_c);
+        __builtin_amdgcn_sched_barrier(0);
+        kv_softmax<HD>(st, s, a.c2, pf);
+        __builtin_amdgcn_sched_barrier(0);
+        values(buf_c);
+        __syncthreads();                               // tile t + 1 is in its buffer, that of t is free
+    };
     const int end_most = cols > 0 ? __builtin_amdgcn_readlane(col.end, cols - 1) : 0;
-    for (; t < t1; ++t) {
-        const int buf = t & 1;
-        copies(t, buf);
+    auto any = [&](int t, auto buf_c) __attribute__((always_inline)) {
+        constexpr int buf = decltype(buf_c)::value;
+        copies(t, buf_c);
         if (t * KV_TILE < end_most) {
-            scores(buf);
+            scores(buf_c);
             int rel[2];
-            const uint32_t there = sh.flags[buf].held;
+            const uint32_t there = t < t_plain ? 0x10101010u : sh.flags[buf].held;
 #pragma unroll
             for (int i = 0; i < 2; ++i) rel[i] = min((int)(there >> (8 * (2 * i + lg)) & 255u), min(max(col.end - (t * KV_TILE + 32 * i + 16 * lg), 0), 16));
             kv_mask(s, rel);
@@ -498,10 +500,23 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            first_values(buf);
-            values(buf);
+            first_values(buf_c);
+            values(buf_c);
         }
         __syncthreads();
+    };
+    constexpr std::integral_constant<int, 0> even{};
+    constexpr std::integral_constant<int, 1> odd{};
+    int t = t0;
+    if (cols > 0) {
+        for (; t + 2 <= t_plain; t += 2) {
+            plain(t, even);
+            plain(t + 1, odd);
+        }
+    }
+    for (; t < t1; t += 2) {
+        any(t, even);
+        if (t + 1 < t1) any(t + 1, odd);
     }
 }
 
@@ -551,59 +566,76 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
     }
 }
 
-// Joins the pieces of the column tiles that have several, in order: a workgroup per 32 columns, a lane per four dims of one.
+// Joins the pieces of the column tiles that shares cut, in order: a workgroup for the first cut of each and 32 columns.  Few columns of many pieces are
+// read by all lanes, G of them for the same four dims of a column, each every G-th piece, and put together in LDS.
 template <int HD, int COLS>
 __global__ __launch_bounds__(256) void kv_join_kernel(AttendArgs a, int most, int least) {
-    const int lane = threadIdx.x & 63;
+    constexpr int QUADS = HD / 4;                              // lanes that a column needs
+    __shared__ float sm[256], part_l[256 / QUADS * 2];
+    __shared__ __attribute__((aligned(16))) floatx4 part[256];
+    const int w1st = blockIdx.x + 1, tid = threadIdx.x;
     const KvShares shares(kv_total<COLS>(a), most, least);
-    if (shares.total == 0) return;
-    // the column tile: sequences in order, then heads
-    int64_t before = 0;
-    int passed = 0;                                            // column tiles of the sequences before base
-    for (int base = 0; base < a.c.n_seqs; base += 64) {
-        const KvScan<COLS> s(a, base);
-        int units = s.s.ct * a.c.heads;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int x = __shfl_up(units, o);
-            units += lane >= o ? x : 0;
+    if (w1st >= shares.wgs) return;
+    const int64_t f = shares.begin(w1st);
+    const KvSeq q = kv_find<COLS>(a, f);
+    const KvPiece p = kv_piece<COLS>(a, q, f, shares.total);
+    const int64_t f0 = q.first + p.h * q.head() + q.before(p.c);
+    const int w0 = w1st - 1, c0 = blockIdx.y * 32, cols = min(32, q.n * a.times - COLS * p.c - c0);
+    if (p.from_start || shares.begin(w0) > f0 || cols <= 0) return;          // no cut, or not the first of this column tile
+    const int wn = shares.of(f0 + q.w0 + (int64_t)p.c * q.dw - 1);
+    auto slot = [&](int w) { return (int64_t)(w == w0 ? 2 * w + 1 : 2 * w) * COLS + c0; };
+    // references: 32 columns x 8 lanes
+    {
+        const int lj = tid & 31;
+        float m = kNoRef;
+        if (lj < cols)
+            for (int w = w0 + (tid >> 5); w <= wn; w += 8) m = fmaxf(m, a.part_ml[(slot(w) + lj) * 2]);
+        sm[tid] = m;
+        __syncthreads();
+        for (int o = 128; o >= 32; o >>= 1) {
+            if (tid < o) sm[tid] = fmaxf(sm[tid], sm[tid + o]);
+            __syncthreads();
         }
-        const int want = (int)blockIdx.x - passed;
-        const uint64_t m = __ballot(want < units);
-        if (!m) {
-            passed += __builtin_amdgcn_readlane(units, 63);
-            before += s.all();
-            continue;
-        }
-        const int l = __builtin_ctzll(m);
-        const KvSeq q = s.pick(a, base, before, l);
-        const int unit = want - (__builtin_amdgcn_readlane(units, l) - q.ct * a.c.heads), h = unit / q.ct, c = unit % q.ct;
-        const int64_t f0 = q.first + h * q.head() + q.before(c);
-        const int w0 = shares.of(f0), w1 = shares.of(f0 + q.w0 + (int64_t)c * q.dw - 1);
-        if (w0 == w1) return;
-        const int c0 = blockIdx.y * 32, cols = min(32, q.n * a.times - COLS * c - c0);
-        for (int i = threadIdx.x; i < cols * (HD / 4); i += 256) {
-            const int lj = i / (HD / 4), d = i % (HD / 4) * 4;
-            auto slot = [&](int w) { return (int64_t)(w == w0 ? 2 * w + 1 : 2 * w) * COLS + c0 + lj; };
-            float mx = kNoRef, sum = 0.0f;
-            for (int w = w0; w <= w1; ++w) mx = fmaxf(mx, a.part_ml[slot(w) * 2]);
-            floatx4 v = {0.f, 0.f, 0.f, 0.f};
-            for (int w = w0; w <= w1; ++w) {
-                const float2 ml = *(const float2*)(a.part_ml + slot(w) * 2);
+    }
+    int G = 1;
+    while (2 * G * cols * QUADS <= 256 && G < wn - w0 + 1) G *= 2;
+    const int lanes = 256 / G;                                 // a multiple of 32; group tid / lanes has every G-th piece
+    for (int i0 = 0; i0 < cols * QUADS; i0 += lanes) {
+        const int i = i0 + tid % lanes, lj = i / QUADS, d = i % QUADS * 4;
+        floatx4 v = {0.f, 0.f, 0.f, 0.f};
+        float sum = 0.0f;
+        if (lj < cols) {
+            const float mx = sm[lj];
+#pragma unroll 4
+            for (int w = w0 + tid / lanes; w <= wn; w += G) {
+                const int64_t at = slot(w) + lj;
+                const float2 ml = *(const float2*)(a.part_ml + at * 2);
+                const floatx4 y = *(const floatx4*)(a.part_o + at * HD + d);
                 const float k = __builtin_amdgcn_exp2f(ml.x - mx);
                 sum = fmaf(ml.y, k, sum);
-                const floatx4 p = *(const floatx4*)(a.part_o + slot(w) * HD + d);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = fmaf(p[e], k, v[e]);
+                for (int e = 0; e < 4; ++e) v[e] = fmaf(y[e], k, v[e]);
             }
-            const float inv = kv_inverse(sum);
-            const KvColumn col = kv_column(a, q, h, COLS * c + c0 + lj);
-            bf16x4 r;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) r[e] = (bf16)(v[e] * inv);
-            *(bf16x4*)(a.o + (int64_t)col.row * a.o_row + (int64_t)col.head * a.o_head + d) = r;
         }
-        return;
+        if (G > 1) {                                           // (then all columns fit in one go)
+            part[tid] = v;
+            if (tid % QUADS == 0) part_l[tid / QUADS] = sum;
+            __syncthreads();
+            if (tid >= lanes) continue;
+            for (int g = 1; g < G; ++g) {
+                const floatx4 y = part[tid + g * lanes];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += y[e];
+                sum += part_l[(tid + g * lanes) / QUADS];
+            }
+        }
+        if (lj >= cols) continue;
+        const float inv = kv_inverse(sum);
+        const KvColumn col = kv_column(a, q, p.h, COLS * p.c + c0 + lj);
+        bf16x4 r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = (bf16)(v[e] * inv);
+        *(bf16x4*)(a.o + (int64_t)col.row * a.o_row + (int64_t)col.head * a.o_head + d) = r;
     }
 }
 
@@ -642,10 +674,10 @@ template <int HD>
 void launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
     if (p.many) {
         hipLaunchKernelGGL((kv_attend_many_kernel<HD, MANY_WAVES>), dim3(p.wgs), dim3(64 * MANY_WAVES), 0, s, a);
-        hipLaunchKernelGGL((kv_join_kernel<HD, 32 * MANY_WAVES>), dim3((unsigned)p.units, MANY_WAVES), dim3(256), 0, s, a, p.wgs, p.least);
+        hipLaunchKernelGGL((kv_join_kernel<HD, 32 * MANY_WAVES>), dim3(p.wgs - 1, MANY_WAVES), dim3(256), 0, s, a, p.wgs, p.least);
     } else {
         hipLaunchKernelGGL(kv_attend_few_kernel<HD>, dim3(p.wgs), dim3(64 * FEW_WAVES), 0, s, a);
-        hipLaunchKernelGGL((kv_join_kernel<HD, 32>), dim3((unsigned)p.units), dim3(256), 0, s, a, p.wgs, p.least);
+        hipLaunchKernelGGL((kv_join_kernel<HD, 32>), dim3(p.wgs - 1), dim3(256), 0, s, a, p.wgs, p.least);
     }
 }
 
