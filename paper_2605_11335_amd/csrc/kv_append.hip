@@ -45,11 +45,6 @@ __device__ __forceinline__ uint32_t moved(uint32_t w, int up) {
     r = __builtin_amdgcn_cvt_pk_fp8_f32(__builtin_ldexpf(b[0], -up), __builtin_ldexpf(b[1], -up), r, true);
     return (uint32_t)r;
 }
-// LDS accesses of this wave before and after it keep their order
-__device__ __forceinline__ void lds_order() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
 __device__ __forceinline__ float wave_max(float m) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));

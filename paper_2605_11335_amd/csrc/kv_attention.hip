@@ -2,7 +2,6 @@
 // sequence's length, of pages that the table does not name and, causal, behind the query take no part, whatever their codes are.
 #include <algorithm>
 #include <cmath>
-#include <type_traits>
 
 #include "context.h"
 #include "kv_tile.h"
@@ -286,16 +285,26 @@ struct ManyFlags {
     uint32_t held;                                     // tokens of each of the tile's groups, a byte each
     uint32_t nan;                                      // t + 1 where a value of tile t was NaN
 };
-template <int HD>
+template <int HD, int NW>
 struct ManyShared {
     bf16x8 k[2][2][HD / 16][64], v[2][4][HD / 32][64];
+    char rows[NW][64 * HD];                            // a wave's query rows on their way to fragments, and its output on the way back
     // of tiles that not every column sees whole:
     uint16_t nan_of[2][4 * HD];                        // which of a V chunk's 16 tokens were NaN
     ManyFlags flags[2];
 };
 
+// Where 16-byte chunk c of a column's row of head_dim values is kept: rows read or written a chunk per lane meet all banks.
+// A value that the compiler takes for a new one: addresses made from it are computed where they are used, and not kept in registers all along.
+__device__ __forceinline__ int anew(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+template <int HD>
+__device__ __forceinline__ int many_row(int col, int c) { return col * (2 * HD) + ((c ^ (col & (HD / 8 - 1))) << 4); }
+
 template <int HD, int NW>
-__device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, int h, int c, int t0, int t1, ManyShared<HD>& sh, KvState<HD>& st) {
+__device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, int h, int c, int t0, int t1, ManyShared<HD, NW>& sh, KvState<HD>& st) {
     constexpr int KS = HD / 16, DT = HD / 32, NT = 64 * NW, GB = 16 * HD;
     constexpr int CHUNKS = 4 * HD, PER = CHUNKS >= NT ? CHUNKS / NT : 1;        // 16-byte chunks of a tile's K; of those and of V's, a lane has PER
     constexpr bool BOTH = CHUNKS >= NT;                                         // else half of the lanes have K, half V
@@ -303,36 +312,49 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
     const int tid = threadIdx.x, lane = tid & 63, lj = lane & 31, lg = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col0 = 32 * NW * c + 32 * wave, cols = min(32, q.n * a.times - col0);            // (cols <= 0: a wave without a column only copies)
     const KvColumn col = kv_column(a, q, h, col0 + lj);
-    st.clear();
-    if (t0 >= t1) return;
+    if (t0 >= t1) {
+        st.clear();
+        return;
+    }
     const int32_t* const table = a.c.table + (int64_t)q.b * a.c.table_stride;
-    // tiles [t0, t_plain) are seen whole by every column of the workgroup and have all their pages
-    const int least = a.causal ? min(q.len, q.len - q.n + 32 * NW * c / a.times + 1) : q.len;
-    int t_plain = max(t0, min(t1, max(least, 0) / KV_TILE));
-    {
-        bool hole = false;
-        for (int p = (t0 * KV_TILE >> a.c.page_shift) + tid; p <= (t_plain * KV_TILE - 1) >> a.c.page_shift; p += NT) hole |= (uint32_t)table[p] >= (uint32_t)a.c.n_pages;
-        if (__syncthreads_or(hole)) t_plain = t0;
-    }
-    bf16x8 qf[KS];
-    {
-        const bf16* const p = a.q + (int64_t)col.row * a.q_row + (int64_t)col.head * a.q_head + 16 * lg;
-#pragma unroll
-        for (int k = 0; k < KS; ++k) qf[k] = *(const bf16x8*)(p + 32 * (k >> 1) + 8 * (k & 1));
-    }
     // ---- copies.  Chunk x of K or V: group x / HD of the tile, 16 bytes x % HD of it.
     const bool has_k = BOTH || tid < CHUNKS, has_v = BOTH || tid >= CHUNKS;
     const int x0 = BOTH ? tid : tid % CHUNKS;
     const int last = q.len - 1, page_mask = (1 << a.c.page_shift) - 1;
-    int page[PER];                                     // of the tile after the one in flight
+    int page[PER], page1[PER];                         // of the tile after the one in flight (page1: of the second tile of all)
     uint32_t pw[PER];                                  // powers of the one in flight
     int held[PER];                                     // how many tokens of its groups there are
     uint32x4 kr[PER], vr[PER];
-    auto look_up = [&](int t) __attribute__((always_inline)) {          // (past the end: some page of the sequence's)
+    auto look_up = [&](int t, int (&page)[PER]) __attribute__((always_inline)) {          // (past the end: some page of the sequence's)
 #pragma unroll
         for (int i = 0; i < PER; ++i) page[i] = table[min(t * KV_TILE + 16 * ((i * NT + x0) / HD), last) >> a.c.page_shift];
     };
-    auto fetch = [&](int t) __attribute__((always_inline)) {
+    // the first loads, none waiting for another: pages of the first tiles, of all tiles (for holes), queries
+    look_up(t0, page);
+    look_up(t0 + 1, page1);
+    if (tid < 2) sh.flags[tid].nan = 0;
+    bf16x8 qf[KS];
+    {
+        const int ln = anew(lane), col_l = ln & 31, half = ln >> 5;
+        bf16x8 x[HD / 16];
+#pragma unroll
+        for (int i = 0; i < HD / 16; ++i) {
+            const KvColumn r = kv_column(a, q, h, col0 + i * (512 / HD) + ln / (HD / 8));
+            x[i] = *(const bf16x8*)(a.q + (int64_t)r.row * a.q_row + (int64_t)r.head * a.q_head + ln % (HD / 8) * 8);
+        }
+#pragma unroll
+        for (int i = 0; i < HD / 16; ++i) *(bf16x8*)(sh.rows[wave] + many_row<HD>(i * (512 / HD) + ln / (HD / 8), ln % (HD / 8))) = x[i];
+        lds_order();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) qf[k] = *(const bf16x8*)(sh.rows[wave] + many_row<HD>(col_l, 4 * (k >> 1) + 2 * half + (k & 1)));
+    }
+    // tiles [t0, t_plain) are seen whole by every column of the workgroup and have all their pages
+    const int least = a.causal ? min(q.len, q.len - q.n + 32 * NW * c / a.times + 1) : q.len;
+    int t_plain = max(t0, min(t1, max(least, 0) / KV_TILE));
+    bool hole = false;
+    for (int p = (t0 * KV_TILE >> a.c.page_shift) + tid; p <= (t_plain * KV_TILE - 1) >> a.c.page_shift; p += NT) hole |= (uint32_t)table[p] >= (uint32_t)a.c.n_pages;
+    auto fetch = [&](int t, const int (&page)[PER]) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int x = i * NT + x0, p = t * KV_TILE + 16 * (x / HD);
@@ -345,8 +367,7 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
             if (has_v) vr[i] = *(const uint32x4*)(a.c.v + (int64_t)g * GB + r);
         }
     };
-    auto convert = [&](int t, auto buf_c) __attribute__((always_inline)) {
-        constexpr int buf = decltype(buf_c)::value;
+    auto convert = [&](int t, int buf) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int x = i * NT + x0, grp = x / HD, r = x % HD;
@@ -380,32 +401,32 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
                 }
             }
             if (has_k) {
-                const int slot = r & 15, ch = r >> 4, row = (slot & 3) | (grp & 1) << 2 | (slot >> 2) << 3, to = row + 32 * (ch & 1);
+                const int slot = r & 15, ch = r >> 4, row = (slot & 3) | (grp & 1) << 2 | (slot >> 2) << 3;
+                bf16x8* const to = &sh.k[0][grp >> 1][ch & ~1][row + 32 * (ch & 1)] + buf * (2 * KS * 64);
                 const float f = kv_power(pk);
-                sh.k[buf][grp >> 1][ch & ~1][to] = kv_wide(kr[i][0], kr[i][1], f);
-                sh.k[buf][grp >> 1][ch | 1][to] = kv_wide(kr[i][2], kr[i][3], f);
+                to[0] = kv_wide(kr[i][0], kr[i][1], f);
+                to[64] = kv_wide(kr[i][2], kr[i][3], f);
             }
             if (has_v) {
-                const int to = (r & 31) + 32 * (grp & 1);
+                bf16x8* const to = &sh.v[0][grp & ~1][r >> 5][(r & 31) + 32 * (grp & 1)] + buf * (4 * DT * 64);
                 const float f = kv_power(pv);
-                sh.v[buf][grp & ~1][r >> 5][to] = kv_wide(vr[i][0], vr[i][1], f);
-                sh.v[buf][grp | 1][r >> 5][to] = kv_wide(vr[i][2], vr[i][3], f);
+                to[0] = kv_wide(vr[i][0], vr[i][1], f);
+                to[DT * 64] = kv_wide(vr[i][2], vr[i][3], f);
             }
         }
     };
     // while a tile is computed: the next one into LDS, the one after on its way
-    auto copies = [&](int t, auto buf_c) __attribute__((always_inline)) {
-        if (t + 1 < t1) convert(t + 1, std::integral_constant<int, 1 - decltype(buf_c)::value>{});
+    auto copies = [&](int t, int buf) __attribute__((always_inline)) {
+        if (t + 1 < t1) convert(t + 1, 1 - buf);
         if (t + 2 < t1) {
-            fetch(t + 2);
-            look_up(t + 3);
+            fetch(t + 2, page);
+            look_up(t + 3, page);
         }
     };
     floatx16 s[2];
     bf16x8 pf[4];
     // S^T = K Q^T: MFMA i has half i & 1 of the keys and k-step i >> 1; fragments run four reads ahead
-    auto scores = [&](auto buf_c) __attribute__((always_inline)) {
-        constexpr int buf = decltype(buf_c)::value;
+    auto scores = [&](int buf) __attribute__((always_inline)) {
         bf16x8 kf[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) kf[i] = sh.k[buf][i & 1][i >> 1][lane];
@@ -427,13 +448,11 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
     };
     // O^T += V^T P^T: MFMA i has k-step i / DT and dims 32 (i % DT) ...; the first fragments are read before the softmax
     bf16x8 vf[4];
-    auto first_values = [&](auto buf_c) __attribute__((always_inline)) {
-        constexpr int buf = decltype(buf_c)::value;
+    auto first_values = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) vf[i] = sh.v[buf][i / DT][i % DT][lane];
     };
-    auto values = [&](auto buf_c) __attribute__((always_inline)) {
-        constexpr int buf = decltype(buf_c)::value;
+    auto values = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 4 * DT; ++i) {
             st.o[i % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i & 3], pf[i / DT], st.o[i % DT], 0, 0, 0);
@@ -446,33 +465,30 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
         }
         __builtin_amdgcn_sched_group_barrier(0x008, 4, 1);
     };
-    if (tid < 2) sh.flags[tid].nan = 0;
-    look_up(t0);
-    fetch(t0);
-    look_up(t0 + 1);
-    __syncthreads();                                   // the flags are cleared (and what the buffers held before has been read)
-    convert(t0, std::integral_constant<int, 0>{});
-    fetch(t0 + 1);
-    look_up(t0 + 2);
+    fetch(t0, page);
+    if (__syncthreads_or(hole)) t_plain = t0;          // (the flags are cleared, too, and what the buffers held before has been read)
+    convert(t0, 0);
+    fetch(t0 + 1, page1);
+    look_up(t0 + 2, page);
+    st.clear();
     __syncthreads();
     // tile t is in buffer (t - t0) & 1
-    auto plain = [&](int t, auto buf_c) __attribute__((always_inline)) {
-        copies(t, buf_c);
+    auto plain = [&](int t, int buf) __attribute__((always_inline)) {
+        copies(t, buf);
         __builtin_amdgcn_sched_barrier(0);
-        scores(buf_c);
-        first_values(buf_c);
+        scores(buf);
+        first_values(buf);
         __builtin_amdgcn_sched_barrier(0);
         kv_softmax<HD>(st, s, a.c2, pf);
         __builtin_amdgcn_sched_barrier(0);
-        values(buf_c);
+        values(buf);
         __syncthreads();                               // tile t + 1 is in its buffer, that of t is free
     };
     const int end_most = cols > 0 ? __builtin_amdgcn_readlane(col.end, cols - 1) : 0;
-    auto any = [&](int t, auto buf_c) __attribute__((always_inline)) {
-        constexpr int buf = decltype(buf_c)::value;
-        copies(t, buf_c);
+    auto any = [&](int t, int buf) __attribute__((always_inline)) {
+        copies(t, buf);
         if (t * KV_TILE < end_most) {
-            scores(buf_c);
+            scores(buf);
             int rel[2];
             const uint32_t there = t < t_plain ? 0x10101010u : sh.flags[buf].held;
 #pragma unroll
@@ -490,41 +506,33 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
 #pragma unroll
                     for (int ks = 0; ks < 4; ++ks) {
                         const uint32_t m = sh.nan_of[buf][(2 * (ks >> 1) + lg) * HD + 32 * d + lj] >> (8 * (ks & 1));
-                        bf16x8 was;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) was[e] = m >> e & 1u ? (bf16)1.0f : (bf16)0.0f;
-                        hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(was, kv_seen(rel[ks >> 1], ks & 1), hits, 0, 0, 0);
+                        hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kv_bits(m), kv_seen(rel[ks >> 1], ks & 1), hits, 0, 0, 0);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                     kv_spread_nan<HD>(st, d, hits);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            first_values(buf_c);
-            values(buf_c);
+            first_values(buf);
+            values(buf);
         }
         __syncthreads();
     };
-    constexpr std::integral_constant<int, 0> even{};
-    constexpr std::integral_constant<int, 1> odd{};
     int t = t0;
     if (cols > 0) {
-        for (; t + 2 <= t_plain; t += 2) {
-            plain(t, even);
-            plain(t + 1, odd);
+        for (; t + 2 <= t_plain; t += 2) {             // (buffers known at compile time: addresses are a lane's offset and a constant)
+            plain(t, 0);
+            plain(t + 1, 1);
         }
     }
-    for (; t < t1; t += 2) {
-        any(t, even);
-        if (t + 1 < t1) any(t + 1, odd);
-    }
+    for (; t < t1; ++t) any(t, (t - t0) & 1);
 }
 
 constexpr int MANY_LEAST = 8 * KV_TILE;                // keys that are worth a workgroup
 template <int HD, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a) {
     constexpr int DT = HD / 32, COLS = 32 * NW;
-    __shared__ ManyShared<HD> sh;
+    __shared__ ManyShared<HD, NW> sh;
     const int lane = threadIdx.x & 63, lj = lane & 31, lg = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const KvShares shares(kv_total<COLS>(a), gridDim.x, MANY_LEAST);
     if ((int)blockIdx.x >= shares.wgs || shares.total == 0) return;
@@ -538,26 +546,37 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
             const KvPiece p = kv_piece<COLS>(a, q, f, f1);
             KvState<HD> st;
             many_sweep<HD, NW>(a, q, p.h, p.c, p.t0, p.t1, sh, st);
-            const KvColumn col = kv_column(a, q, p.h, COLS * p.c + 32 * wave + lj);
+            const int col0 = COLS * p.c + 32 * wave, cols = min(32, q.n * a.times - col0);
             const float l = st.l + __shfl_xor(st.l, 32);
-            if (col.mine) {
-                if (p.whole) {
-                    const float inv = kv_inverse(l);
-                    bf16* const to = a.o + (int64_t)col.row * a.o_row + (int64_t)col.head * a.o_head + 4 * lg;
+            if (cols > 0 && p.whole) {
+                // rows of 2 head_dim bytes, 16 per lane: stored by dims of a lane, an instruction would touch 32 rows (13640 queries x 24 heads: 60 us of stores)
+                const float inv = kv_inverse(l);
+                const int ln = anew(lane), col_l = ln & 31, half = ln >> 5;
 #pragma unroll
-                    for (int i = 0; i < DT * 4; ++i) {
-                        bf16x4 r;
+                for (int i = 0; i < DT * 4; ++i) {
+                    bf16x4 r;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) r[e] = (bf16)(st.o[i / 4][i % 4 * 4 + e] * inv);
-                        *(bf16x4*)(to + 8 * i) = r;
-                    }
-                } else {
-                    const int64_t at = (int64_t)(2 * w + p.from_start) * COLS + 32 * wave + lj;
-                    float* const to = a.part_o + at * HD + 4 * lg;
+                    for (int e = 0; e < 4; ++e) r[e] = (bf16)(st.o[i / 4][i % 4 * 4 + e] * inv);
+                    *(bf16x4*)(sh.rows[wave] + many_row<HD>(col_l, i) + 8 * half) = r;
+                }
+                lds_order();
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < HD / 16; ++i) {
+                    const int r = i * (512 / HD) + ln / (HD / 8), ch = ln % (HD / 8);
+                    const KvColumn to = kv_column(a, q, p.h, col0 + r);
+                    const bf16x8 x = *(const bf16x8*)(sh.rows[wave] + many_row<HD>(r, ch));
+                    if (r < cols) *(bf16x8*)(a.o + (int64_t)to.row * a.o_row + (int64_t)to.head * a.o_head + ch * 8) = x;
+                }
+                lds_order();
+            } else if (cols > 0) {
+                const int64_t at = (int64_t)(2 * w + p.from_start) * NW + wave;
+                if (lj < cols) {
+                    float* const to = a.part_o + at * (HD / 8) * 256 + lane * 4;
 #pragma unroll
                     for (int i = 0; i < DT * 4; ++i)
-                        *(floatx4*)(to + 8 * i) = floatx4{st.o[i / 4][i % 4 * 4], st.o[i / 4][i % 4 * 4 + 1], st.o[i / 4][i % 4 * 4 + 2], st.o[i / 4][i % 4 * 4 + 3]};
-                    if (lg == 0) *(float2*)(a.part_ml + at * 2) = make_float2(st.mc, l);
+                        *(floatx4*)(to + i * 256) = floatx4{st.o[i / 4][i % 4 * 4], st.o[i / 4][i % 4 * 4 + 1], st.o[i / 4][i % 4 * 4 + 2], st.o[i / 4][i % 4 * 4 + 3]};
+                    if (lg == 0) *(float2*)(a.part_ml + (at * 32 + lj) * 2) = make_float2(st.mc, l);
                 }
             }
             __syncthreads();                           // the next piece's tiles go where this one's were
@@ -571,7 +590,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
 template <int HD, int COLS>
 __global__ __launch_bounds__(256) void kv_join_kernel(AttendArgs a, int most, int least) {
     constexpr int QUADS = HD / 4;                              // lanes that a column needs
-    __shared__ float sm[256], part_l[256 / QUADS * 2];
+    __shared__ float sm[256], part_l[16 * 32];                 // G is 256 / QUADS at most, with one column
     __shared__ __attribute__((aligned(16))) floatx4 part[256];
     const int w1st = blockIdx.x + 1, tid = threadIdx.x;
     const KvShares shares(kv_total<COLS>(a), most, least);
@@ -583,13 +602,13 @@ __global__ __launch_bounds__(256) void kv_join_kernel(AttendArgs a, int most, in
     const int w0 = w1st - 1, c0 = blockIdx.y * 32, cols = min(32, q.n * a.times - COLS * p.c - c0);
     if (p.from_start || shares.begin(w0) > f0 || cols <= 0) return;          // no cut, or not the first of this column tile
     const int wn = shares.of(f0 + q.w0 + (int64_t)p.c * q.dw - 1);
-    auto slot = [&](int w) { return (int64_t)(w == w0 ? 2 * w + 1 : 2 * w) * COLS + c0; };
+    auto slot = [&](int w) { return (int64_t)(w == w0 ? 2 * w + 1 : 2 * w) * (COLS / 32) + blockIdx.y; };
     // references: 32 columns x 8 lanes
     {
         const int lj = tid & 31;
         float m = kNoRef;
         if (lj < cols)
-            for (int w = w0 + (tid >> 5); w <= wn; w += 8) m = fmaxf(m, a.part_ml[(slot(w) + lj) * 2]);
+            for (int w = w0 + (tid >> 5); w <= wn; w += 8) m = fmaxf(m, a.part_ml[(slot(w) * 32 + lj) * 2]);
         sm[tid] = m;
         __syncthreads();
         for (int o = 128; o >= 32; o >>= 1) {
@@ -601,16 +620,18 @@ __global__ __launch_bounds__(256) void kv_join_kernel(AttendArgs a, int most, in
     while (2 * G * cols * QUADS <= 256 && G < wn - w0 + 1) G *= 2;
     const int lanes = 256 / G;                                 // a multiple of 32; group tid / lanes has every G-th piece
     for (int i0 = 0; i0 < cols * QUADS; i0 += lanes) {
-        const int i = i0 + tid % lanes, lj = i / QUADS, d = i % QUADS * 4;
+        const int i = i0 + tid % lanes;
+        const int lj = COLS == 32 ? i / QUADS : i % cols, quad = COLS == 32 ? i % QUADS : i / cols;           // column, its dims 4 quad ..
         floatx4 v = {0.f, 0.f, 0.f, 0.f};
         float sum = 0.0f;
-        if (lj < cols) {
+        const bool some = lj < cols && quad < QUADS;
+        if (some) {
             const float mx = sm[lj];
 #pragma unroll 4
             for (int w = w0 + tid / lanes; w <= wn; w += G) {
-                const int64_t at = slot(w) + lj;
-                const float2 ml = *(const float2*)(a.part_ml + at * 2);
-                const floatx4 y = *(const floatx4*)(a.part_o + at * HD + d);
+                const int64_t at = slot(w);
+                const float2 ml = *(const float2*)(a.part_ml + (at * 32 + lj) * 2);
+                const floatx4 y = *(const floatx4*)(a.part_o + (COLS == 32 ? (at * 32 + lj) * HD + 4 * quad : (at * (HD / 8) + (quad >> 1)) * 256 + (lj + 32 * (quad & 1)) * 4));
                 const float k = __builtin_amdgcn_exp2f(ml.x - mx);
                 sum = fmaf(ml.y, k, sum);
 #pragma unroll
@@ -619,23 +640,23 @@ __global__ __launch_bounds__(256) void kv_join_kernel(AttendArgs a, int most, in
         }
         if (G > 1) {                                           // (then all columns fit in one go)
             part[tid] = v;
-            if (tid % QUADS == 0) part_l[tid / QUADS] = sum;
+            if (quad == 0 && some) part_l[tid / lanes * 32 + lj] = sum;
             __syncthreads();
             if (tid >= lanes) continue;
             for (int g = 1; g < G; ++g) {
                 const floatx4 y = part[tid + g * lanes];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] += y[e];
-                sum += part_l[(tid + g * lanes) / QUADS];
+                sum += part_l[g * 32 + lj];
             }
         }
-        if (lj >= cols) continue;
+        if (!some) continue;
         const float inv = kv_inverse(sum);
         const KvColumn col = kv_column(a, q, p.h, COLS * p.c + c0 + lj);
         bf16x4 r;
 #pragma unroll
         for (int e = 0; e < 4; ++e) r[e] = (bf16)(v[e] * inv);
-        *(bf16x4*)(a.o + (int64_t)col.row * a.o_row + (int64_t)col.head * a.o_head + d) = r;
+        *(bf16x4*)(a.o + (int64_t)col.row * a.o_row + (int64_t)col.head * a.o_head + 4 * quad) = r;
     }
 }
 

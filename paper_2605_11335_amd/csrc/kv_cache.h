@@ -30,6 +30,12 @@ __device__ __forceinline__ int kv_group(const KvView& c, int b, int h, int p) {
 // Offsets of a ragged batch are the caller's device memory: whatever they hold, rows stay within [0, n_rows).
 __device__ __forceinline__ int kv_clamped(int x, int lo, int hi) { return min(max(x, lo), hi); }
 
+// LDS accesses of this wave before and after it keep their order.
+__device__ __forceinline__ void lds_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // Host checks of a cache; NULL if it is in order.
 inline const char* kv_bad(const cf_kv_cache* c) {
     if (!c) return "null cache";

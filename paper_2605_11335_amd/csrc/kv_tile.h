@@ -24,8 +24,9 @@ struct AttendArgs {
     int32_t n_tokens, heads, times;        // times: query heads per key head
     int32_t causal;
     float c2;                              // scale * log2(e)
-    float* part_o;                         // results of parts of a column tile's keys: [slot][column][head_dim], then
-    float* part_ml;                        // [slot][column][2]: reference (base 2) and sum of the weights
+    float* part_o;                         // results of pieces of a column tile's keys: few columns [column][head_dim], many as they lie in registers,
+                                           // [32 columns][head_dim / 8][lane][4]; then
+    float* part_ml;                        // [column][2]: reference (base 2) and sum of the weights
 };
 
 constexpr int KV_TILE = 64;                // keys
@@ -254,12 +255,15 @@ __device__ __forceinline__ uint32_t kv_nan_codes(uint32_t w) { return ((w & 0x7f
 __device__ __forceinline__ uint32_t kv_perhaps_nan(uint32_t w) { return (~w & 0x7f7f7f7fu) - 0x01010101u; }
 __device__ __forceinline__ uint32_t kv_without_nan(uint32_t w, uint32_t nans) { return w & ~((nans << 1) - (nans >> 7)); }
 __device__ __forceinline__ uint32_t kv_ones(uint32_t nans) { return (nans >> 7) * 0x38u; }                                          // the code of 1
-__device__ __forceinline__ bf16x8 kv_seen(int rel, int u) {
-    bf16x8 r;
+// 1 for each of eight bits
+__device__ __forceinline__ bf16x8 kv_bits(uint32_t m) {
+    uint32x4 r;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = 8 * u + e < rel ? (bf16)1.0f : (bf16)0.0f;
-    return r;
+    for (int i = 0; i < 4; ++i) r[i] = ((m >> (2 * i) & 1u) | (m << (15 - 2 * i) & 0x10000u)) * 0x3f80u;
+    return __builtin_bit_cast(bf16x8, r);
 }
+// which of a lane's keys 8u .. 8u + 7 of a half its column sees
+__device__ __forceinline__ bf16x8 kv_seen(int rel, int u) { return kv_bits((1u << rel) - 1u >> (8 * u)); }
 template <int HD>
 __device__ __forceinline__ void kv_spread_nan(KvState<HD>& st, int d, const floatx16& hits) {
 #pragma unroll
