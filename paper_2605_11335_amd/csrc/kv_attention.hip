@@ -216,14 +216,16 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attend_few_kernel(Attend
     __shared__ bf16x8 sq[HD / 16][64];                      // query fragments, the same for all waves
     const int lane = threadIdx.x & 63, lj = lane & 31, lg = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = blockIdx.x;
     const KvShares shares(kv_total<32>(a), gridDim.x, FEW_LEAST);
-    if (w >= shares.wgs || shares.total == 0) return;
-    int64_t f = shares.begin(w);
-    const int64_t f1 = shares.begin(w + 1);
+    KvSeq q = {};
+    KvPiece p = {};
+    const bool any = w < shares.wgs && shares.total > 0;
+    int64_t f = any ? shares.begin(w) : 0;
+    const int64_t f1 = any ? shares.begin(w + 1) : 0;
     while (f < f1) {
-        const KvSeq q = kv_find<32>(a, f);
+        q = kv_find<32>(a, f);
         const int64_t q_end = q.first + q.head() * a.c.heads;
         while (f < f1 && f < q_end) {
-            const KvPiece p = kv_piece<32>(a, q, f, f1);
+            p = kv_piece<32>(a, q, f, f1);
             const int h = p.h, c = p.c;
             const KvColumn col = kv_column(a, q, h, 32 * c + lj);
             for (int k = wave; k < HD / 16; k += FEW_WAVES)
@@ -274,6 +276,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attend_few_kernel(Attend
             f = p.next;
         }
     }
+    kv_leave_cut<32>(a, shares, w, q, p, any);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -535,15 +538,17 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
     __shared__ ManyShared<HD, NW> sh;
     const int lane = threadIdx.x & 63, lj = lane & 31, lg = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const KvShares shares(kv_total<COLS>(a), gridDim.x, MANY_LEAST);
-    if ((int)blockIdx.x >= shares.wgs || shares.total == 0) return;
-    const int w = (int)xcd_contiguous_id(blockIdx.x, shares.wgs);         // neighbours in the work, which share keys, on one XCD
-    int64_t f = shares.begin(w);
-    const int64_t f1 = shares.begin(w + 1);
+    KvSeq q = {};
+    KvPiece p = {};
+    const bool any = (int)blockIdx.x < shares.wgs && shares.total > 0;
+    const int w = any ? (int)xcd_contiguous_id(blockIdx.x, shares.wgs) : (int)blockIdx.x;         // neighbours in the work, which share keys, on one XCD
+    int64_t f = any ? shares.begin(w) : 0;
+    const int64_t f1 = any ? shares.begin(w + 1) : 0;
     while (f < f1) {
-        const KvSeq q = kv_find<COLS>(a, f);
+        q = kv_find<COLS>(a, f);
         const int64_t q_end = q.first + q.head() * a.c.heads;
         while (f < f1 && f < q_end) {
-            const KvPiece p = kv_piece<COLS>(a, q, f, f1);
+            p = kv_piece<COLS>(a, q, f, f1);
             KvState<HD> st;
             many_sweep<HD, NW>(a, q, p.h, p.c, p.t0, p.t1, sh, st);
             const int col0 = COLS * p.c + 32 * wave, cols = min(32, q.n * a.times - col0);
@@ -583,81 +588,112 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
             f = p.next;
         }
     }
+    kv_leave_cut<COLS>(a, shares, w, q, p, any);
 }
 
-// Joins the pieces of the column tiles that shares cut, in order: a workgroup for the first cut of each and 32 columns.  Few columns of many pieces are
-// read by all lanes, G of them for the same four dims of a column, each every G-th piece, and put together in LDS.
-template <int HD, int COLS>
-__global__ __launch_bounds__(256) void kv_join_kernel(AttendArgs a, int most, int least) {
-    constexpr int QUADS = HD / 4;                              // lanes that a column needs
-    __shared__ float sm[256], part_l[16 * 32];                 // G is 256 / QUADS at most, with one column
-    __shared__ __attribute__((aligned(16))) floatx4 part[256];
-    const int w1st = blockIdx.x + 1, tid = threadIdx.x;
-    const KvShares shares(kv_total<COLS>(a), most, least);
-    if (w1st >= shares.wgs) return;
-    const int64_t f = shares.begin(w1st);
-    const KvSeq q = kv_find<COLS>(a, f);
-    const KvPiece p = kv_piece<COLS>(a, q, f, shares.total);
-    const int64_t f0 = q.first + p.h * q.head() + q.before(p.c);
-    const int w0 = w1st - 1, c0 = blockIdx.y * 32, cols = min(32, q.n * a.times - COLS * p.c - c0);
-    if (p.from_start || shares.begin(w0) > f0 || cols <= 0) return;          // no cut, or not the first of this column tile
-    const int wn = shares.of(f0 + q.w0 + (int64_t)p.c * q.dw - 1);
-    auto slot = [&](int w) { return (int64_t)(w == w0 ? 2 * w + 1 : 2 * w) * (COLS / 32) + blockIdx.y; };
-    // references: 32 columns x 8 lanes
+// Joins the pieces of the column tiles that shares cut, in order: a workgroup per cut and 32 columns.  Bound by latency: what to join has been left in
+// memory by who cut it, and all of a lane's loads are on their way at once.  Few columns of many pieces are read by all lanes, G of them for the same
+// four dims of a column, each every G-th piece, and put together in LDS.
+template <int HD, int COLS, int LANES>
+__global__ __launch_bounds__(LANES) void kv_join_kernel(AttendArgs a) {
+    constexpr int QUADS = HD / 4, TIMES = 32 * QUADS / LANES > 1 ? 32 * QUADS / LANES : 1;      // lanes that a column needs; columns x quads per lane
+    __shared__ float sm[LANES], part_l[LANES / QUADS * 32];
+    __shared__ __attribute__((aligned(16))) floatx4 part[LANES];
+    const int tid = threadIdx.x, w0 = blockIdx.x;
+    const KvCut cut = a.cuts[w0];
+    const int c0 = blockIdx.y * 32, cols = min(32, cut.n * a.times - cut.col0 - c0), pieces = cut.pieces;
+    if (pieces == 0 || cols <= 0) return;
+    KvSeq q = {};
+    q.start = cut.start;
+    q.n = cut.n;
+    auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * w0 + 1 : 2 * (w0 + i)) * (COLS / 32) + blockIdx.y; };         // of the i-th piece
+    auto load = [&](int i, int lj, int quad) {
+        return *(const floatx4*)(a.part_o + (COLS == 32 ? (slot(i) * 32 + lj) * HD + 4 * quad : (slot(i) * (HD / 8) + (quad >> 1)) * 256 + (lj + 32 * (quad & 1)) * 4));
+    };
+    auto store = [&](int lj, int quad, const floatx4& v, float sum) {
+        const float inv = kv_inverse(sum);
+        const KvColumn col = kv_column(a, q, cut.h, cut.col0 + c0 + lj);
+        bf16x4 r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = (bf16)(v[e] * inv);
+        *(bf16x4*)(a.o + (int64_t)col.row * a.o_row + (int64_t)col.head * a.o_head + 4 * quad) = r;
+    };
+    // references: 32 columns x LANES / 32
     {
         const int lj = tid & 31;
         float m = kNoRef;
         if (lj < cols)
-            for (int w = w0 + (tid >> 5); w <= wn; w += 8) m = fmaxf(m, a.part_ml[(slot(w) * 32 + lj) * 2]);
+            for (int i = tid >> 5; i < pieces; i += LANES / 32) m = fmaxf(m, a.part_ml[(slot(i) * 32 + lj) * 2]);
         sm[tid] = m;
         __syncthreads();
-        for (int o = 128; o >= 32; o >>= 1) {
+        for (int o = LANES / 2; o >= 32; o >>= 1) {
             if (tid < o) sm[tid] = fmaxf(sm[tid], sm[tid + o]);
             __syncthreads();
         }
     }
     int G = 1;
-    while (2 * G * cols * QUADS <= 256 && G < wn - w0 + 1) G *= 2;
-    const int lanes = 256 / G;                                 // a multiple of 32; group tid / lanes has every G-th piece
-    for (int i0 = 0; i0 < cols * QUADS; i0 += lanes) {
-        const int i = i0 + tid % lanes;
-        const int lj = COLS == 32 ? i / QUADS : i % cols, quad = COLS == 32 ? i % QUADS : i / cols;           // column, its dims 4 quad ..
-        floatx4 v = {0.f, 0.f, 0.f, 0.f};
-        float sum = 0.0f;
-        const bool some = lj < cols && quad < QUADS;
-        if (some) {
-            const float mx = sm[lj];
-#pragma unroll 4
-            for (int w = w0 + tid / lanes; w <= wn; w += G) {
-                const int64_t at = slot(w);
-                const float2 ml = *(const float2*)(a.part_ml + (at * 32 + lj) * 2);
-                const floatx4 y = *(const floatx4*)(a.part_o + (COLS == 32 ? (at * 32 + lj) * HD + 4 * quad : (at * (HD / 8) + (quad >> 1)) * 256 + (lj + 32 * (quad & 1)) * 4));
-                const float k = __builtin_amdgcn_exp2f(ml.x - mx);
-                sum = fmaf(ml.y, k, sum);
+    while (2 * G * cols * QUADS <= LANES && G < pieces) G *= 2;
+    if (G == 1) {
+        floatx4 v[TIMES];
+        float sum[TIMES];
+        int lj[TIMES], quad[TIMES];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = fmaf(y[e], k, v[e]);
+        for (int k = 0; k < TIMES; ++k) {
+            const int x = min(k * LANES + tid, cols * QUADS - 1);           // (past the end: the last one again)
+            lj[k] = COLS == 32 ? x / QUADS : x % cols;
+            quad[k] = COLS == 32 ? x % QUADS : x / cols;
+            v[k] = floatx4{0.f, 0.f, 0.f, 0.f};
+            sum[k] = 0.0f;
+        }
+#pragma unroll 2
+        for (int i = 0; i < pieces; ++i) {
+            floatx4 y[TIMES];
+            float2 ml[TIMES];
+#pragma unroll
+            for (int k = 0; k < TIMES; ++k) {
+                y[k] = load(i, lj[k], quad[k]);
+                ml[k] = *(const float2*)(a.part_ml + (slot(i) * 32 + lj[k]) * 2);
+            }
+#pragma unroll
+            for (int k = 0; k < TIMES; ++k) {
+                const float f = __builtin_amdgcn_exp2f(ml[k].x - sm[lj[k]]);
+                sum[k] = fmaf(ml[k].y, f, sum[k]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[k][e] = fmaf(y[k][e], f, v[k][e]);
             }
         }
-        if (G > 1) {                                           // (then all columns fit in one go)
-            part[tid] = v;
-            if (quad == 0 && some) part_l[tid / lanes * 32 + lj] = sum;
-            __syncthreads();
-            if (tid >= lanes) continue;
-            for (int g = 1; g < G; ++g) {
-                const floatx4 y = part[tid + g * lanes];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] += y[e];
-                sum += part_l[g * 32 + lj];
-            }
-        }
-        if (!some) continue;
-        const float inv = kv_inverse(sum);
-        const KvColumn col = kv_column(a, q, p.h, COLS * p.c + c0 + lj);
-        bf16x4 r;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) r[e] = (bf16)(v[e] * inv);
-        *(bf16x4*)(a.o + (int64_t)col.row * a.o_row + (int64_t)col.head * a.o_head + 4 * quad) = r;
+        for (int k = 0; k < TIMES; ++k)
+            if (k * LANES + tid < cols * QUADS) store(lj[k], quad[k], v[k], sum[k]);
+        return;
     }
+    const int lanes = LANES / G, g = tid / lanes, x = tid % lanes;           // lanes: a multiple of 16
+    const int lj = COLS == 32 ? x / QUADS : x % cols, quad = COLS == 32 ? x % QUADS : x / cols;
+    const bool some = x < cols * QUADS;
+    floatx4 v = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.0f;
+    if (some) {
+#pragma unroll 4
+        for (int i = g; i < pieces; i += G) {
+            const floatx4 y = load(i, lj, quad);
+            const float2 ml = *(const float2*)(a.part_ml + (slot(i) * 32 + lj) * 2);
+            const float f = __builtin_amdgcn_exp2f(ml.x - sm[lj]);
+            sum = fmaf(ml.y, f, sum);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = fmaf(y[e], f, v[e]);
+        }
+        part[tid] = v;
+        if (quad == 0) part_l[g * 32 + lj] = sum;
+    }
+    __syncthreads();
+    if (!some || g > 0) return;
+    for (int k = 1; k < G; ++k) {
+        const floatx4 y = part[tid + k * lanes];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += y[e];
+        sum += part_l[k * 32 + lj];
+    }
+    store(lj, quad, v, sum);
 }
 
 const char* query_bad(const cf_kv_cache* c, const cf_kv_query* x) {
@@ -671,9 +707,9 @@ constexpr int FEW_WGS = 512, MANY_WGS = 256;           // two workgroups on each
 
 struct AttendPlan {
     bool many;                         // kernel with MANY_WAVES * 32 columns per workgroup
-    int cols, wgs, least;
+    int cols, wgs;
     int64_t units;                     // column tiles of all sequences and key heads, at most
-    uint64_t ml_offset, bytes;         // of the workspace
+    uint64_t ml_offset, cuts_offset, bytes;         // of the workspace
 };
 constexpr int MANY_WAVES = 8;
 const char* attend_plan(const cf_kv_cache* c, const cf_kv_query* x, AttendPlan* p) {
@@ -682,12 +718,12 @@ const char* attend_plan(const cf_kv_cache* c, const cf_kv_query* x, AttendPlan* 
     p->many = most > 32;
     p->cols = p->many ? 32 * MANY_WAVES : 32;
     p->wgs = p->many ? MANY_WGS : FEW_WGS;
-    p->least = p->many ? MANY_LEAST : FEW_LEAST;
     p->units = (all / p->cols + std::min(c->n_seqs, x->n_tokens)) * c->heads;
     if (p->units > 0x7fffffff) return "too many queries";
     const uint64_t slots = 2ull * p->wgs * p->cols;
     p->ml_offset = slots * c->head_dim * 4;
-    p->bytes = p->ml_offset + slots * 2 * 4;
+    p->cuts_offset = p->ml_offset + slots * 2 * 4;
+    p->bytes = p->cuts_offset + p->wgs * sizeof(KvCut);
     return nullptr;
 }
 
@@ -695,10 +731,10 @@ template <int HD>
 void launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
     if (p.many) {
         hipLaunchKernelGGL((kv_attend_many_kernel<HD, MANY_WAVES>), dim3(p.wgs), dim3(64 * MANY_WAVES), 0, s, a);
-        hipLaunchKernelGGL((kv_join_kernel<HD, 32 * MANY_WAVES>), dim3(p.wgs - 1, MANY_WAVES), dim3(256), 0, s, a, p.wgs, p.least);
+        hipLaunchKernelGGL((kv_join_kernel<HD, 32 * MANY_WAVES, 256>), dim3(p.wgs - 1, MANY_WAVES), dim3(256), 0, s, a);
     } else {
         hipLaunchKernelGGL(kv_attend_few_kernel<HD>, dim3(p.wgs), dim3(64 * FEW_WAVES), 0, s, a);
-        hipLaunchKernelGGL((kv_join_kernel<HD, 32>), dim3(p.wgs - 1), dim3(256), 0, s, a, p.wgs, p.least);
+        hipLaunchKernelGGL((kv_join_kernel<HD, 32, 1024>), dim3(p.wgs - 1), dim3(1024), 0, s, a);
     }
 }
 
@@ -738,6 +774,7 @@ extern "C" int cf_kv_attention(const cf_kv_cache* cache, const cf_kv_query* x, v
         return cf_fail(nullptr, CF_ERR_ARG, "kv_attention: a workspace of %llu bytes, 256-byte aligned, is needed", (unsigned long long)p.bytes);
     a.part_o = (float*)workspace;
     a.part_ml = (float*)((char*)workspace + p.ml_offset);
+    a.cuts = (KvCut*)((char*)workspace + p.cuts_offset);
     hipStream_t s = (hipStream_t)stream;
     if (cache->head_dim == 128) launch<128>(a, p, s);
     else launch<64>(a, p, s);

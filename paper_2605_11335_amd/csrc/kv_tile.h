@@ -27,6 +27,11 @@ struct AttendArgs {
     float* part_o;                         // results of pieces of a column tile's keys: few columns [column][head_dim], many as they lie in registers,
                                            // [32 columns][head_dim / 8][lane][4]; then
     float* part_ml;                        // [column][2]: reference (base 2) and sum of the weights
+    struct KvCut* cuts;                    // [workgroups]
+};
+// A column tile whose first piece is the last one of a share: query rows of its sequence, key head, first column, how many pieces (0: no such tile).
+struct KvCut {
+    int32_t start, n, h, col0, pieces, pad[3];
 };
 
 constexpr int KV_TILE = 64;                // keys
@@ -157,6 +162,21 @@ struct KvShares {
         return w;
     }
 };
+
+// What the last piece of a workgroup's share (and that of a workgroup without one) leaves for the kernel that joins pieces.
+template <int COLS>
+__device__ __forceinline__ void kv_leave_cut(const AttendArgs& a, const KvShares& shares, int w, const KvSeq& q, const KvPiece& p, bool any) {
+    KvCut cut = {};
+    if (any && p.from_start && !p.whole) {
+        const int64_t unit = q.first + p.h * q.head() + q.before(p.c);
+        cut.start = q.start;
+        cut.n = q.n;
+        cut.h = p.h;
+        cut.col0 = COLS * p.c;
+        cut.pieces = shares.of(unit + q.w0 + (int64_t)p.c * q.dw - 1) - w + 1;
+    }
+    if (threadIdx.x == 0) a.cuts[w] = cut;
+}
 
 // A lane's column of a column tile.
 struct KvColumn {
