@@ -11,6 +11,7 @@ import os
 from typing import Dict, List, Optional
 
 import numpy as np
+import torch                 # before the library: PyTorch ships its own HIP runtime, and two of them in one process do not share the device
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libchunkflow.so")
@@ -139,9 +140,6 @@ def lib() -> C.CDLL:
         if not os.path.exists(LIB_PATH):
             raise ImportError(f"{LIB_PATH} is missing: build it with `python paper_2605_11335_amd/build.py` "
                               "(there is no CPU or PyTorch fallback for the block path)")
-        # PyTorch ships its own HIP runtime; load it first so that this library binds to the same
-        # one (two runtimes in one process do not share the device)
-        import torch  # noqa: F401
         _lib = C.CDLL(LIB_PATH)
         _lib.cf_last_error.restype = C.c_char_p
         _lib.cf_last_error.argtypes = [C.c_void_p]
@@ -516,7 +514,7 @@ def cf_op_checksum_noalloc(data, nbytes, first_word, dev_out, stream=None) -> No
 
 # ---- rotary positions.  The calls from here on look at their tensors' types, shapes, strides and devices, run on the device the tensors are on
 # and, without a stream, on torch's current one there.
-_TYPES: dict = {}
+_TYPES = {torch.bfloat16: CF_BF16, torch.float32: CF_F32}
 
 
 def _refuse(cond, msg: str) -> None:
@@ -528,29 +526,26 @@ def _refuse(cond, msg: str) -> None:
 def _dtype_of(t) -> int:
     code = _TYPES.get(t.dtype)
     if code is None:
-        import torch
-        _TYPES.update({torch.bfloat16: CF_BF16, torch.float32: CF_F32})
-        code = _TYPES.get(t.dtype)
-        if code is None:
-            raise ChunkflowError(CF_ERR_ARG, f"{t.dtype} is neither bfloat16 nor float32")
+        raise ChunkflowError(CF_ERR_ARG, f"{t.dtype} is neither bfloat16 nor float32")
     return code
 
 
 def _launch(fn, name: str, device, stream, *args) -> None:
     """fn(*args, stream) on `device`, which has to be a GPU."""
-    import torch
     if device.type != "cuda":
         raise ChunkflowError(CF_ERR_ARG, f"{name}: tensors on {device}, not on a GPU")
-    cuda, index = torch.cuda, device.index
+    index = device.index
     if stream is None:
-        stream = cuda.current_stream(index)
+        handle = torch._C._cuda_getCurrentRawStream(index)          # (of torch.cuda.current_stream, without making a Stream: 0.2 of 2 us)
     elif stream.device_index != index:
         raise ChunkflowError(CF_ERR_ARG, f"{name}: a stream of GPU {stream.device_index} for tensors on {device}")
-    if cuda.current_device() == index:
-        rc = fn(*args, stream.cuda_stream)
     else:
-        with cuda.device(index):
-            rc = fn(*args, stream.cuda_stream)
+        handle = stream.cuda_stream
+    if torch.cuda.current_device() == index:
+        rc = fn(*args, handle)
+    else:
+        with torch.cuda.device(index):
+            rc = fn(*args, handle)
     if rc != 0:
         _check(rc)
 
@@ -578,7 +573,6 @@ def cf_rope_plan(head_dim: int, axis_pairs, theta=10000.0) -> cf_rope:
 
 def cf_rope_tables(rope: cf_rope, pos, cos_out, sin_out, stream=None) -> None:
     """cos_out, sin_out [n, head_dim / 2] float32 of pos [n, axes] int32: what cf_block_io takes as rope_cos and rope_sin."""
-    import torch
     n = pos.shape[0]
     p = _dense(pos, "rope_tables: pos", torch.int32, (n, rope.n_axes))
     c = _dense(cos_out, "rope_tables: cos_out", torch.float32, (n, rope.head_dim // 2), pos.device)
@@ -609,7 +603,6 @@ def _rope_operand(rope, x, y, n, like, which) -> tuple:
 def cf_rope_apply(rope: cf_rope, pos, q, q_out, k=None, k_out=None, inverse: bool = False, stream=None) -> None:
     """q_out = q [n, heads, head_dim] turned by pos [n, axes] int32 (inverse: turned back, the gradient), and k likewise if given; in place
     where the output is the input."""
-    import torch
     n = q.shape[0]
     p = _dense(pos, "rope_apply: pos", torch.int32, (n, rope.n_axes), q.device)
     _refuse((k is None) != (k_out is None), "rope_apply: k and k_out go together")
@@ -625,7 +618,6 @@ class KVCache:
     """Handle of a paged cache for cf_kv_append and cf_kv_attention (make_kv_cache); keeps its tensors alive."""
 
     def __init__(self, k, v, scales, table):
-        import torch
         _refuse(k.dim() != 6 or tuple(k.shape[4:]) != (16, 16), f"kv_cache: k has shape {tuple(k.shape)}, expected [pages, heads, page / 16, head_dim / 16, 16, 16]")
         pages, heads, groups, chunks = k.shape[:4]
         codes = (torch.uint8, torch.float8_e4m3fn)
@@ -647,13 +639,11 @@ def make_kv_cache(k, v, scales, table) -> KVCache:
 
 def _batch(cache, what: str, cu, lens) -> tuple:
     """Pointers of offsets [sequences + 1] and lengths [sequences]."""
-    import torch
     return _dense(cu, what, torch.int32, (cache.n_seqs + 1,), cache.device), _dense(lens, what, torch.int32, (cache.n_seqs,), cache.device)
 
 
 def cf_kv_append(cache: KVCache, k, v, cu, lens, rope: Optional[cf_rope] = None, pos=None, stream=None) -> None:
     """Rows cu[b] .. cu[b+1] of k and v [tokens, heads, head_dim] (bf16 or fp32) become tokens lens[b], ... of sequence b, k turned by pos if a plan is given."""
-    import torch
     n, want = k.shape[0], (cache.heads, cache.head_dim)
     if k.dim() != 3 or k.shape[1:] != want or v.shape != k.shape:
         raise ChunkflowError(CF_ERR_ARG, f"kv_append: k {tuple(k.shape)} and v {tuple(v.shape)}, expected [tokens, {want[0]}, {want[1]}]")
@@ -678,7 +668,6 @@ def cf_kv_attention_workspace(cache: KVCache, q, max_q: int = 0) -> int:
 def cf_kv_attention(cache: KVCache, q, o, cu, lens, causal: bool = False, scale: Optional[float] = None, max_q: int = 0, workspace=None, stream=None) -> None:
     """o = softmax(scale q K^T) V for rows cu[b] .. cu[b+1] of q [tokens, heads, head_dim] (bf16) over the first lens[b] tokens of sequence b; scale: 1 / sqrt(head_dim)
     if not given.  workspace: a dense tensor of cf_kv_attention_workspace bytes."""
-    import torch
     n = q.shape[0]
     if q.dim() != 3 or q.shape[2] != cache.head_dim or o.shape != q.shape:
         raise ChunkflowError(CF_ERR_ARG, f"kv_attention: q {tuple(q.shape)} and o {tuple(o.shape)}, expected [tokens, heads, {cache.head_dim}]")

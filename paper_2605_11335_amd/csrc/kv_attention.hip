@@ -13,7 +13,7 @@ namespace {
 // memory into registers, each wave its own tiles, K of the next tile on its way while this one's second half is computed and V behind it: up to
 // 16 KB in flight per wave.  All key tiles of the batch laid end to end are cut into equal parts, one per workgroup, wherever sequences and heads
 // begin and end; a column tile whose keys lie in several parts is joined by kv_join_kernel.
-constexpr int FEW_WAVES = 4, FEW_LEAST = 4 * KV_TILE;           // FEW_LEAST: keys that are worth a workgroup
+constexpr int FEW_WAVES = 4, FEW_LEAST = 5 * KV_TILE;           // FEW_LEAST: weight that is worth a workgroup
 
 // One column tile of 32 over key tiles [t0, t1), of which each wave takes every FEW_WAVES-th: its own result.  Tiles that every column sees whole
 // come first, one after the other without a break in the loads; then those with an end, a hole in the page table or a power that is none, if there are any.
@@ -215,7 +215,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attend_few_kernel(Attend
     __shared__ float sm[FEW_WAVES][32][2];
     __shared__ bf16x8 sq[HD / 16][64];                      // query fragments, the same for all waves
     const int lane = threadIdx.x & 63, lj = lane & 31, lg = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = blockIdx.x;
-    const KvShares shares(kv_total<32>(a), gridDim.x, FEW_LEAST);
+    const KvShares shares(kv_total<32>(a), gridDim.x, a.whole ? 1 : FEW_LEAST);
     KvSeq q = {};
     KvPiece p = {};
     const bool any = w < shares.wgs && shares.total > 0;
@@ -276,7 +276,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attend_few_kernel(Attend
             f = p.next;
         }
     }
-    kv_leave_cut<32>(a, shares, w, q, p, any);
+    if (!a.whole) kv_leave_cut<32>(a, shares, w, q, p, any);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -531,13 +531,13 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
     for (; t < t1; ++t) any(t, (t - t0) & 1);
 }
 
-constexpr int MANY_LEAST = 8 * KV_TILE;                // keys that are worth a workgroup
+constexpr int MANY_LEAST = 8 * KV_TILE;                // weight that is worth a workgroup
 template <int HD, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a) {
     constexpr int DT = HD / 32, COLS = 32 * NW;
     __shared__ ManyShared<HD, NW> sh;
     const int lane = threadIdx.x & 63, lj = lane & 31, lg = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const KvShares shares(kv_total<COLS>(a), gridDim.x, MANY_LEAST);
+    const KvShares shares(kv_total<COLS>(a), gridDim.x, a.whole ? 1 : MANY_LEAST);
     KvSeq q = {};
     KvPiece p = {};
     const bool any = (int)blockIdx.x < shares.wgs && shares.total > 0;
@@ -588,7 +588,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
             f = p.next;
         }
     }
-    kv_leave_cut<COLS>(a, shares, w, q, p, any);
+    if (!a.whole) kv_leave_cut<COLS>(a, shares, w, q, p, any);
 }
 
 // Joins the pieces of the column tiles that shares cut, in order: a workgroup per cut and 32 columns.  Bound by latency: what to join has been left in
@@ -705,7 +705,25 @@ const char* query_bad(const cf_kv_cache* c, const cf_kv_query* x) {
 
 constexpr int FEW_WGS = 512, MANY_WGS = 256;           // two workgroups on each CU, one
 
+// Whether column tiles are left whole, a workgroup to each, and nothing has to be joined.  `tiles`: of the longest sequence the table has room for, which
+// is all that the host knows.
+// Few columns: as long as all column tiles run at once and their keys, FEW_WAVES tiles at a time, take little longer than shares of them would, and
+// six such steps for the joining.  One query each, 8 key heads, whole / cut: 1 sequence of 1024 tokens 11.9 / 13.1 us, of 2048 16.4 / 12.9; 16 of 2048
+// 17.9 / 22.2, 64 of 2048 52.7 / 55.1; 256 of 512 74.8 / 61.8.
+bool few_whole(int64_t units, int64_t tiles) {
+    const int64_t steps = (tiles + FEW_WAVES - 1) / FEW_WAVES;
+    return units <= FEW_WGS && steps <= steps * units / FEW_WGS + 6;
+}
+// Many: 1.9 us per tile and 12 for the ends of a column tile, in whole rounds of workgroups, against equal shares and 25 us for leaving and joining their
+// pieces.  24 heads, whole / cut: 2560 queries x 2048 keys 74 / 98 us, 5461 x 512 73 / 77, 5461 x 2048 187 / 167, 10922 x 2048 313 / 293,
+// 21845 x 512 213 / 207, 43690 x 512 385 / 370.
+bool many_whole(int64_t units, int64_t tiles) {
+    const double one = 12.0 + 1.9 * (double)tiles, rounds = (double)((units + MANY_WGS - 1) / MANY_WGS);
+    return rounds * one <= (double)units * one / MANY_WGS + 25.0;
+}
+
 struct AttendPlan {
+    bool whole;                        // a workgroup per column tile
     bool many;                         // kernel with MANY_WAVES * 32 columns per workgroup
     int cols, wgs;
     int64_t units;                     // column tiles of all sequences and key heads, at most
@@ -720,10 +738,13 @@ const char* attend_plan(const cf_kv_cache* c, const cf_kv_query* x, AttendPlan* 
     p->wgs = p->many ? MANY_WGS : FEW_WGS;
     p->units = (all / p->cols + std::min(c->n_seqs, x->n_tokens)) * c->heads;
     if (p->units > 0x7fffffff) return "too many queries";
-    const uint64_t slots = 2ull * p->wgs * p->cols;
+    const int64_t tiles = ((int64_t)c->table_width * c->page_tokens + KV_TILE - 1) / KV_TILE;
+    p->whole = p->many ? many_whole(p->units, tiles) : few_whole(p->units, tiles);
+    if (p->whole) p->wgs = (int)p->units;
+    const uint64_t slots = p->whole ? 0 : 2ull * p->wgs * p->cols;
     p->ml_offset = slots * c->head_dim * 4;
     p->cuts_offset = p->ml_offset + slots * 2 * 4;
-    p->bytes = p->cuts_offset + p->wgs * sizeof(KvCut);
+    p->bytes = p->whole ? 0 : p->cuts_offset + p->wgs * sizeof(KvCut);
     return nullptr;
 }
 
@@ -731,10 +752,10 @@ template <int HD>
 void launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
     if (p.many) {
         hipLaunchKernelGGL((kv_attend_many_kernel<HD, MANY_WAVES>), dim3(p.wgs), dim3(64 * MANY_WAVES), 0, s, a);
-        hipLaunchKernelGGL((kv_join_kernel<HD, 32 * MANY_WAVES, 256>), dim3(p.wgs - 1, MANY_WAVES), dim3(256), 0, s, a);
+        if (!p.whole) hipLaunchKernelGGL((kv_join_kernel<HD, 32 * MANY_WAVES, 256>), dim3(p.wgs - 1, MANY_WAVES), dim3(256), 0, s, a);
     } else {
         hipLaunchKernelGGL(kv_attend_few_kernel<HD>, dim3(p.wgs), dim3(64 * FEW_WAVES), 0, s, a);
-        hipLaunchKernelGGL((kv_join_kernel<HD, 32, 1024>), dim3(p.wgs - 1), dim3(1024), 0, s, a);
+        if (!p.whole) hipLaunchKernelGGL((kv_join_kernel<HD, 32, 1024>), dim3(p.wgs - 1), dim3(1024), 0, s, a);
     }
 }
 
@@ -770,8 +791,9 @@ extern "C" int cf_kv_attention(const cf_kv_cache* cache, const cf_kv_query* x, v
     a.c2 = x->scale * 1.4426950408889634f;
     AttendPlan p;
     if (const char* bad = attend_plan(cache, x, &p)) return cf_fail(nullptr, CF_ERR_ARG, "kv_attention: %s", bad);
-    if (!workspace || (uintptr_t)workspace % 256 || workspace_bytes < p.bytes)
+    if (p.bytes && (!workspace || (uintptr_t)workspace % 256 || workspace_bytes < p.bytes))
         return cf_fail(nullptr, CF_ERR_ARG, "kv_attention: a workspace of %llu bytes, 256-byte aligned, is needed", (unsigned long long)p.bytes);
+    a.whole = p.whole;
     a.part_o = (float*)workspace;
     a.part_ml = (float*)((char*)workspace + p.ml_offset);
     a.cuts = (KvCut*)((char*)workspace + p.cuts_offset);

@@ -23,6 +23,7 @@ struct AttendArgs {
     const int32_t *cu, *lens;
     int32_t n_tokens, heads, times;        // times: query heads per key head
     int32_t causal;
+    int32_t whole;                         // no column tile is cut: each is a share of its own
     float c2;                              // scale * log2(e)
     float* part_o;                         // results of pieces of a column tile's keys: few columns [column][head_dim], many as they lie in registers,
                                            // [32 columns][head_dim / 8][lane][4]; then
@@ -37,7 +38,8 @@ struct KvCut {
 constexpr int KV_TILE = 64;                // keys
 
 // Work is laid end to end -- sequences, in each the key heads, in each the column tiles of COLS columns -- and cut into equal shares wherever that is.
-// The weight of a column tile is about the number of keys that it goes through: w0 + c dw for the c-th of a sequence (dw = 0 unless causal).
+// The weight of a column tile is about the number of keys that it goes through, and as many as its beginning and end take the time of: w0 + c dw for
+// the c-th of a sequence (dw = 0 unless causal).
 struct KvSeq {
     int b, start, n, len, ct;              // ct: column tiles
     int w0, dw;
@@ -53,11 +55,14 @@ __device__ __forceinline__ int64_t kv_lane64(int64_t x, int lane) {
 template <int COLS>
 __device__ __forceinline__ void kv_weigh(const AttendArgs& a, KvSeq& s) {
     s.ct = (s.n * a.times + COLS - 1) / COLS;
-    s.w0 = max(KV_TILE, s.len);            // (columns that see nothing have to be set to zero)
+    constexpr int ENDS = COLS == 32 ? 4 * KV_TILE : 6 * KV_TILE;           // 5 us of a workgroup alone, 12 us with all of them at their queries and outputs
+    s.w0 = s.len + ENDS;
     s.dw = 0;
-    if (a.causal && s.ct > 1) {
+    if (a.whole) {
+        s.w0 = 1;
+    } else if (a.causal && s.ct > 1) {
         s.dw = COLS / a.times;             // query rows from one column tile to the next
-        s.w0 = max(KV_TILE, s.len - s.n + s.dw);
+        s.w0 = max(0, s.len - s.n) + s.dw + ENDS;
     }
 }
 // The sequence of each lane, i = base + lane, and the inclusive sum of the work up to it.
