@@ -291,73 +291,58 @@ struct ManyFlags {
 template <int HD, int NW>
 struct ManyShared {
     bf16x8 k[2][2][HD / 16][64], v[2][4][HD / 32][64];
-    char rows[NW][64 * HD];                            // a wave's query rows on their way to fragments, and its output on the way back
+    char rows[NW][64 * HD];                            // a wave's query rows, as many_row has them, on their way to fragments
     // of tiles that not every column sees whole:
     uint16_t nan_of[2][4 * HD];                        // which of a V chunk's 16 tokens were NaN
     ManyFlags flags[2];
 };
 
-// Where 16-byte chunk c of a column's row of head_dim values is kept: rows read or written a chunk per lane meet all banks.
 // A value that the compiler takes for a new one: addresses made from it are computed where they are used, and not kept in registers all along.
 __device__ __forceinline__ int anew(int x) {
     asm volatile("" : "+v"(x));
     return x;
 }
+// Where 16-byte chunk c of a column's row of head_dim values is kept: rows read or written a chunk per lane meet all banks.
 template <int HD>
 __device__ __forceinline__ int many_row(int col, int c) { return col * (2 * HD) + ((c ^ (col & (HD / 8 - 1))) << 4); }
 
+// What is on its way for the workgroup's next piece while it finishes one.
 template <int HD, int NW>
-__device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, int h, int c, int t0, int t1, ManyShared<HD, NW>& sh, KvState<HD>& st) {
-    constexpr int KS = HD / 16, DT = HD / 32, NT = 64 * NW, GB = 16 * HD;
-    constexpr int CHUNKS = 4 * HD, PER = CHUNKS >= NT ? CHUNKS / NT : 1;        // 16-byte chunks of a tile's K; of those and of V's, a lane has PER
+struct ManyAhead {
+    static constexpr int CHUNKS = 4 * HD, NT = 64 * NW;                         // 16-byte chunks of a tile's K or V
+    static constexpr int PER = CHUNKS >= NT ? CHUNKS / NT : 1;                  // of those and of V's, a lane has PER
+    int page1[PER];                                    // pages of its second tile
+    uint32_t pw[PER];                                  // the first tile's powers,
+    int held[PER];                                     // how many tokens of its groups there are,
+    uint32x4 kr[PER], vr[PER];                         // and its codes
+};
+
+// Piece p of sequence q.  ready: its query rows are in LDS, its first codes on their way (x).  more: piece n of the same sequence comes next, and is made ready.
+template <int HD, int NW>
+__device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, const KvPiece& p, bool holes, bool ready, const KvPiece& n, bool more,
+                                           ManyShared<HD, NW>& sh, ManyAhead<HD, NW>& x, KvState<HD>& st) {
+    constexpr int KS = HD / 16, DT = HD / 32, NT = 64 * NW, GB = 16 * HD, CHUNKS = 4 * HD, PER = ManyAhead<HD, NW>::PER;
     constexpr bool BOTH = CHUNKS >= NT;                                         // else half of the lanes have K, half V
     static_assert(CHUNKS % NT == 0 || 2 * CHUNKS == NT, "");
     const int tid = threadIdx.x, lane = tid & 63, lj = lane & 31, lg = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int col0 = 32 * NW * c + 32 * wave, cols = min(32, q.n * a.times - col0);            // (cols <= 0: a wave without a column only copies)
-    const KvColumn col = kv_column(a, q, h, col0 + lj);
-    if (t0 >= t1) {
-        st.clear();
-        return;
-    }
+    const int t0 = p.t0, t1 = p.t1;
+    const int col0 = 32 * NW * p.c + 32 * wave, cols = min(32, q.n * a.times - col0);          // (cols <= 0: a wave without a column only copies)
+    const KvColumn col = kv_column(a, q, p.h, col0 + lj);
     const int32_t* const table = a.c.table + (int64_t)q.b * a.c.table_stride;
     // ---- copies.  Chunk x of K or V: group x / HD of the tile, 16 bytes x % HD of it.
     const bool has_k = BOTH || tid < CHUNKS, has_v = BOTH || tid >= CHUNKS;
     const int x0 = BOTH ? tid : tid % CHUNKS;
     const int last = q.len - 1, page_mask = (1 << a.c.page_shift) - 1;
-    int page[PER], page1[PER];                         // of the tile after the one in flight (page1: of the second tile of all)
-    uint32_t pw[PER];                                  // powers of the one in flight
-    int held[PER];                                     // how many tokens of its groups there are
-    uint32x4 kr[PER], vr[PER];
+    int page[PER];                                     // of the tile after the one in flight
+    auto& pw = x.pw;
+    auto& held = x.held;
+    auto& kr = x.kr;
+    auto& vr = x.vr;
     auto look_up = [&](int t, int (&page)[PER]) __attribute__((always_inline)) {          // (past the end: some page of the sequence's)
 #pragma unroll
         for (int i = 0; i < PER; ++i) page[i] = table[min(t * KV_TILE + 16 * ((i * NT + x0) / HD), last) >> a.c.page_shift];
     };
-    // the first loads, none waiting for another: pages of the first tiles, of all tiles (for holes), queries
-    look_up(t0, page);
-    look_up(t0 + 1, page1);
-    if (tid < 2) sh.flags[tid].nan = 0;
-    bf16x8 qf[KS];
-    {
-        const int ln = anew(lane), col_l = ln & 31, half = ln >> 5;
-        bf16x8 x[HD / 16];
-#pragma unroll
-        for (int i = 0; i < HD / 16; ++i) {
-            const KvColumn r = kv_column(a, q, h, col0 + i * (512 / HD) + ln / (HD / 8));
-            x[i] = *(const bf16x8*)(a.q + (int64_t)r.row * a.q_row + (int64_t)r.head * a.q_head + ln % (HD / 8) * 8);
-        }
-#pragma unroll
-        for (int i = 0; i < HD / 16; ++i) *(bf16x8*)(sh.rows[wave] + many_row<HD>(i * (512 / HD) + ln / (HD / 8), ln % (HD / 8))) = x[i];
-        lds_order();
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int k = 0; k < KS; ++k) qf[k] = *(const bf16x8*)(sh.rows[wave] + many_row<HD>(col_l, 4 * (k >> 1) + 2 * half + (k & 1)));
-    }
-    // tiles [t0, t_plain) are seen whole by every column of the workgroup and have all their pages
-    const int least = a.causal ? min(q.len, q.len - q.n + 32 * NW * c / a.times + 1) : q.len;
-    int t_plain = max(t0, min(t1, max(least, 0) / KV_TILE));
-    bool hole = false;
-    for (int p = (t0 * KV_TILE >> a.c.page_shift) + tid; p <= (t_plain * KV_TILE - 1) >> a.c.page_shift; p += NT) hole |= (uint32_t)table[p] >= (uint32_t)a.c.n_pages;
-    auto fetch = [&](int t, const int (&page)[PER]) __attribute__((always_inline)) {
+    auto fetch = [&](int h, int t, const int (&page)[PER]) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int x = i * NT + x0, p = t * KV_TILE + 16 * (x / HD);
@@ -370,6 +355,43 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
             if (has_v) vr[i] = *(const uint32x4*)(a.c.v + (int64_t)g * GB + r);
         }
     };
+    // this wave's query rows from memory into LDS, past the registers: a lane fetches the chunk whose place it fills
+    auto ask_queries = [&](const KvPiece& p) __attribute__((always_inline)) {
+        const int ln = anew(lane), col0 = 32 * NW * p.c + 32 * wave;
+#pragma unroll
+        for (int i = 0; i < HD / 16; ++i) {
+            const int r = i * (512 / HD) + ln / (HD / 8), ch = ln % (HD / 8) ^ (r & (HD / 8 - 1));
+            const KvColumn c = kv_column(a, q, p.h, col0 + r);
+            const bf16* const from = a.q + (int64_t)c.row * a.q_row + (int64_t)c.head * a.q_head + ch * 8;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                             (__attribute__((address_space(3))) void*)(sh.rows[wave] + i * 1024), 16, 0, 0);
+        }
+    };
+    auto landed = []() __attribute__((always_inline)) { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
+    if (tid < 2) sh.flags[tid].nan = 0;
+    // tiles [t0, t_plain) are seen whole by every column of the workgroup and have all their pages
+    const int least = a.causal ? min(q.len, q.len - q.n + 32 * NW * p.c / a.times + 1) : q.len;
+    int t_plain = max(t0, min(t1, max(least, 0) / KV_TILE));
+    if (!ready) {
+        look_up(t0, page);
+        look_up(t0 + 1, x.page1);
+        ask_queries(p);
+        fetch(p.h, t0, page);
+        landed();
+    }
+    bf16x8 qf[KS];
+    {
+        const int ln = anew(lane), col_l = ln & 31, half = ln >> 5;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) qf[k] = *(const bf16x8*)(sh.rows[wave] + many_row<HD>(col_l, 4 * (k >> 1) + 2 * half + (k & 1)));
+    }
+    if (holes) {                                       // somewhere in the sequence: here?
+        bool hole = false;
+        for (int i = (t0 * KV_TILE >> a.c.page_shift) + tid; i <= (t_plain * KV_TILE - 1) >> a.c.page_shift; i += NT) hole |= (uint32_t)table[i] >= (uint32_t)a.c.n_pages;
+        if (__syncthreads_or(hole)) t_plain = t0;
+    } else {
+        __syncthreads();                               // the flags are cleared, and what the buffers held before has been read
+    }
     auto convert = [&](int t, int buf) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
@@ -422,7 +444,7 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
     auto copies = [&](int t, int buf) __attribute__((always_inline)) {
         if (t + 1 < t1) convert(t + 1, 1 - buf);
         if (t + 2 < t1) {
-            fetch(t + 2, page);
+            fetch(p.h, t + 2, page);
             look_up(t + 3, page);
         }
     };
@@ -468,13 +490,17 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
         }
         __builtin_amdgcn_sched_group_barrier(0x008, 4, 1);
     };
-    fetch(t0, page);
-    if (__syncthreads_or(hole)) t_plain = t0;          // (the flags are cleared, too, and what the buffers held before has been read)
     convert(t0, 0);
-    fetch(t0 + 1, page1);
+    fetch(p.h, t0 + 1, x.page1);
     look_up(t0 + 2, page);
     st.clear();
     __syncthreads();
+    int next_page[PER];
+    if (more) {                                        // (every wave has its queries in registers)
+        look_up(n.t0, next_page);
+        look_up(n.t0 + 1, x.page1);
+        ask_queries(n);
+    }
     // tile t is in buffer (t - t0) & 1
     auto plain = [&](int t, int buf) __attribute__((always_inline)) {
         copies(t, buf);
@@ -529,6 +555,10 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
         }
     }
     for (; t < t1; ++t) any(t, (t - t0) & 1);
+    if (more) {
+        landed();                                      // the queries
+        fetch(n.h, n.t0, next_page);
+    }
 }
 
 constexpr int MANY_LEAST = 8 * KV_TILE;                // weight that is worth a workgroup
@@ -546,23 +576,39 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
     const int64_t f1 = any ? shares.begin(w + 1) : 0;
     while (f < f1) {
         q = kv_find<COLS>(a, f);
-        const int64_t q_end = q.first + q.head() * a.c.heads;
-        while (f < f1 && f < q_end) {
-            p = kv_piece<COLS>(a, q, f, f1);
+        const int64_t q_end = min(f1, q.first + q.head() * a.c.heads);
+        bool hole = false;
+        for (int i = threadIdx.x; i <= (q.len - 1) >> a.c.page_shift; i += 64 * NW) hole |= (uint32_t)a.c.table[(int64_t)q.b * a.c.table_stride + i] >= (uint32_t)a.c.n_pages;
+        const bool holes = __syncthreads_or(hole);
+        ManyAhead<HD, NW> ahead;
+        KvPiece n = kv_piece<COLS>(a, q, f, f1);
+        for (bool ready = false; f < q_end;) {
+            p = n;
+            bool more = p.next < q_end;
+            if (more) n = kv_piece<COLS>(a, q, p.next, f1);
+            more = more && n.t0 < n.t1;
             KvState<HD> st;
-            many_sweep<HD, NW>(a, q, p.h, p.c, p.t0, p.t1, sh, st);
+            if (p.t0 < p.t1) {
+                many_sweep<HD, NW>(a, q, p, holes, ready, n, more, sh, ahead, st);
+                ready = more;
+            } else {
+                st.clear();
+                ready = false;
+            }
             const int col0 = COLS * p.c + 32 * wave, cols = min(32, q.n * a.times - col0);
             const float l = st.l + __shfl_xor(st.l, 32);
             if (cols > 0 && p.whole) {
                 // rows of 2 head_dim bytes, 16 per lane: stored by dims of a lane, an instruction would touch 32 rows (13640 queries x 24 heads: 60 us of stores)
                 const float inv = kv_inverse(l);
                 const int ln = anew(lane), col_l = ln & 31, half = ln >> 5;
+                char* const rows = (char*)&sh.k + wave * (64 * HD);            // where tiles were: k and v are as large as the outputs
+                static_assert(sizeof(sh.k) + sizeof(sh.v) >= NW * 64 * HD, "");
 #pragma unroll
                 for (int i = 0; i < DT * 4; ++i) {
                     bf16x4 r;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) r[e] = (bf16)(st.o[i / 4][i % 4 * 4 + e] * inv);
-                    *(bf16x4*)(sh.rows[wave] + many_row<HD>(col_l, i) + 8 * half) = r;
+                    *(bf16x4*)(rows + many_row<HD>(col_l, i) + 8 * half) = r;
                 }
                 lds_order();
                 __builtin_amdgcn_sched_barrier(0);
@@ -570,7 +616,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
                 for (int i = 0; i < HD / 16; ++i) {
                     const int r = i * (512 / HD) + ln / (HD / 8), ch = ln % (HD / 8);
                     const KvColumn to = kv_column(a, q, p.h, col0 + r);
-                    const bf16x8 x = *(const bf16x8*)(sh.rows[wave] + many_row<HD>(r, ch));
+                    const bf16x8 x = *(const bf16x8*)(rows + many_row<HD>(r, ch));
                     if (r < cols) *(bf16x8*)(a.o + (int64_t)to.row * a.o_row + (int64_t)to.head * a.o_head + ch * 8) = x;
                 }
                 lds_order();
@@ -584,7 +630,6 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
                     if (lg == 0) *(float2*)(a.part_ml + (at * 32 + lj) * 2) = make_float2(st.mc, l);
                 }
             }
-            __syncthreads();                           // the next piece's tiles go where this one's were
             f = p.next;
         }
     }
