@@ -1,6 +1,8 @@
 // Softmax attention of ragged queries over a paged 8-bit cache (kv_cache.h).  Each group's codes are multiplied by its power of two; keys past a
 // sequence's length, of pages that the table does not name and, causal, behind the query take no part, whatever their codes are.
 #include <algorithm>
+#include <atomic>
+#include <chrono>
 #include <cmath>
 
 #include "context.h"
@@ -317,6 +319,9 @@ struct ManyAhead {
     uint32x4 kr[PER], vr[PER];                         // and its codes
 };
 
+constexpr int AGENT = 16;                              // cache policy of a buffer access: sc1, past the XCD's L2
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t agent_rsrc(const void* base, int bytes) { return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00020000); }
+
 // Piece p of sequence q.  ready: its query rows are in LDS, its first codes on their way (x).  more: piece n of the same sequence comes next, and is made ready.
 template <int HD, int NW>
 __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, const KvPiece& p, bool holes, bool ready, const KvPiece& n, bool more,
@@ -574,6 +579,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
     const int w = any ? (int)xcd_contiguous_id(blockIdx.x, shares.wgs) : (int)blockIdx.x;         // neighbours in the work, which share keys, on one XCD
     int64_t f = any ? shares.begin(w) : 0;
     const int64_t f1 = any ? shares.begin(w + 1) : 0;
+    bool joined = false;                               // the last piece, with what follows it
     while (f < f1) {
         q = kv_find<COLS>(a, f);
         const int64_t q_end = min(f1, q.first + q.head() * a.c.heads);
@@ -596,8 +602,26 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
                 ready = false;
             }
             const int col0 = COLS * p.c + 32 * wave, cols = min(32, q.n * a.times - col0);
-            const float l = st.l + __shfl_xor(st.l, 32);
-            if (cols > 0 && p.whole) {
+            float l = st.l + __shfl_xor(st.l, 32);
+            // A column tile of two pieces: the share after this one began with the other, so that it is nearly always there; if so, it is joined here, in the
+            // order and with the roundings of kv_join_kernel.
+            if (cols > 0 && p.from_start && !p.whole && p.end <= shares.begin(w + 2) &&
+                __hip_atomic_load(a.sent + (w + 1) * NW + wave, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.epoch) {
+                asm volatile("" ::: "memory");
+                const int64_t at = (int64_t)(2 * (w + 1)) * NW + wave;
+                const __amdgpu_buffer_rsrc_t part = agent_rsrc(a.part_o + at * (HD / 8) * 256, HD / 8 * 1024), part_ml = agent_rsrc(a.part_ml + at * 64, 256);
+                const float2 ml = __builtin_bit_cast(float2, __builtin_amdgcn_raw_buffer_load_b64(part_ml, (anew(lane) & 31) * 8, 0, AGENT));
+                const float m = fmaxf(fmaxf(kNoRef, st.mc), ml.x), k0 = __builtin_amdgcn_exp2f(st.mc - m), k1 = __builtin_amdgcn_exp2f(ml.x - m);
+                l = fmaf(ml.y, k1, l * k0);
+#pragma unroll
+                for (int i = 0; i < DT * 4; ++i) {
+                    const floatx4 y = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(part, anew(lane) * 16, i * 1024, AGENT));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) st.o[i / 4][i % 4 * 4 + e] = fmaf(y[e], k1, __fmul_rn(st.o[i / 4][i % 4 * 4 + e], k0));
+                }
+                joined = true;
+            }
+            if (cols > 0 && (p.whole || joined)) {
                 // rows of 2 head_dim bytes, 16 per lane: stored by dims of a lane, an instruction would touch 32 rows (13640 queries x 24 heads: 60 us of stores)
                 const float inv = kv_inverse(l);
                 const int ln = anew(lane), col_l = ln & 31, half = ln >> 5;
@@ -622,18 +646,26 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
                 lds_order();
             } else if (cols > 0) {
                 const int64_t at = (int64_t)(2 * w + p.from_start) * NW + wave;
-                if (lj < cols) {
-                    float* const to = a.part_o + at * (HD / 8) * 256 + lane * 4;
+                // past this XCD's L2, for the workgroup that may join it within the launch
+                const __amdgpu_buffer_rsrc_t part = agent_rsrc(a.part_o + at * (HD / 8) * 256, HD / 8 * 1024), part_ml = agent_rsrc(a.part_ml + at * 64, 256);
 #pragma unroll
-                    for (int i = 0; i < DT * 4; ++i)
-                        *(floatx4*)(to + i * 256) = floatx4{st.o[i / 4][i % 4 * 4], st.o[i / 4][i % 4 * 4 + 1], st.o[i / 4][i % 4 * 4 + 2], st.o[i / 4][i % 4 * 4 + 3]};
-                    if (lg == 0) *(float2*)(a.part_ml + (at * 32 + lj) * 2) = make_float2(st.mc, l);
+                for (int i = 0; i < DT * 4; ++i) {
+                    const floatx4 v = {st.o[i / 4][i % 4 * 4], st.o[i / 4][i % 4 * 4 + 1], st.o[i / 4][i % 4 * 4 + 2], st.o[i / 4][i % 4 * 4 + 3]};
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint32x4, v), part, anew(lane) * 16, i * 1024, AGENT);
+                }
+                if (lg == 0) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(uint32x2, make_float2(st.mc, l)), part_ml, lj * 8, 0, AGENT);
+                if (!p.from_start) {
+                    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // all of it is there
+                    if (lane == 0) __hip_atomic_store(a.sent + w * NW + wave, a.epoch, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                 }
             }
             f = p.next;
         }
     }
-    if (!a.whole) kv_leave_cut<COLS>(a, shares, w, q, p, any);
+    if (!a.whole) {
+        kv_leave_cut<COLS>(a, shares, w, q, p, any);
+        if (lane == 0) a.joined[w * NW + wave] = joined;
+    }
 }
 
 // Joins the pieces of the column tiles that shares cut, in order: a workgroup per cut and 32 columns.  Bound by latency: what to join has been left in
@@ -646,6 +678,10 @@ __global__ __launch_bounds__(LANES) void kv_join_kernel(AttendArgs a) {
     __shared__ __attribute__((aligned(16))) floatx4 part[LANES];
     const int tid = threadIdx.x, w0 = blockIdx.x;
     const KvCut cut = a.cuts[w0];
+    if (COLS > 32) {                                           // (many columns)
+        if (tid == 0) a.sent[(w0 + 1) * (COLS / 32) + blockIdx.y] = 0;
+        if (a.joined[w0 * (COLS / 32) + blockIdx.y]) return;
+    }
     const int c0 = blockIdx.y * 32, cols = min(32, cut.n * a.times - cut.col0 - c0), pieces = cut.pieces;
     if (pieces == 0 || cols <= 0) return;
     KvSeq q = {};
@@ -772,7 +808,7 @@ struct AttendPlan {
     bool many;                         // kernel with MANY_WAVES * 32 columns per workgroup
     int cols, wgs;
     int64_t units;                     // column tiles of all sequences and key heads, at most
-    uint64_t ml_offset, cuts_offset, bytes;         // of the workspace
+    uint64_t ml_offset, cuts_offset, sent_offset, bytes;         // of the workspace
 };
 constexpr int MANY_WAVES = 8;
 const char* attend_plan(const cf_kv_cache* c, const cf_kv_query* x, AttendPlan* p) {
@@ -789,8 +825,20 @@ const char* attend_plan(const cf_kv_cache* c, const cf_kv_query* x, AttendPlan* 
     const uint64_t slots = p->whole ? 0 : 2ull * p->wgs * p->cols;
     p->ml_offset = slots * c->head_dim * 4;
     p->cuts_offset = p->ml_offset + slots * 2 * 4;
-    p->bytes = p->whole ? 0 : p->cuts_offset + p->wgs * sizeof(KvCut);
+    p->sent_offset = p->cuts_offset + p->wgs * sizeof(KvCut);
+    p->bytes = p->whole ? 0 : p->sent_offset + (p->many ? p->wgs * MANY_WAVES * (8 + 4) : 0);
     return nullptr;
+}
+
+// A number that no earlier call has had and that memory holds by chance no more often than any other of 64 bits.  (Replays of a captured call have
+// the same one: they find the words at 0, as the call before left them.)
+unsigned long long next_epoch() {
+    static std::atomic<unsigned long long> calls{(unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count() << 20};
+    unsigned long long z = calls.fetch_add(1, std::memory_order_relaxed) * 0x9E3779B97F4A7C15ull;
+    z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+    z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+    z ^= z >> 31;
+    return z ? z : 1;
 }
 
 template <int HD>
@@ -842,6 +890,9 @@ extern "C" int cf_kv_attention(const cf_kv_cache* cache, const cf_kv_query* x, v
     a.part_o = (float*)workspace;
     a.part_ml = (float*)((char*)workspace + p.ml_offset);
     a.cuts = (KvCut*)((char*)workspace + p.cuts_offset);
+    a.sent = (unsigned long long*)((char*)workspace + p.sent_offset);
+    a.joined = (uint32_t*)(a.sent + p.wgs * MANY_WAVES);
+    a.epoch = next_epoch();
     hipStream_t s = (hipStream_t)stream;
     if (cache->head_dim == 128) launch<128>(a, p, s);
     else launch<64>(a, p, s);

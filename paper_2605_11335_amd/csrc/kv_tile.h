@@ -29,6 +29,11 @@ struct AttendArgs {
                                            // [32 columns][head_dim / 8][lane][4]; then
     float* part_ml;                        // [column][2]: reference (base 2) and sum of the weights
     struct KvCut* cuts;                    // [workgroups]
+    // Many columns, [workgroups][waves]: whether the first piece of a share is there for all to see (`epoch` says so; whatever else is in memory does not,
+    // and the kernel that joins pieces leaves 0), and whether its last one has been joined with what follows.
+    unsigned long long* sent;
+    uint32_t* joined;
+    unsigned long long epoch;
 };
 // A column tile whose first piece is the last one of a share: query rows of its sequence, key head, first column, how many pieces (0: no such tile).
 struct KvCut {
@@ -120,7 +125,7 @@ __device__ __forceinline__ KvSeq kv_find(const AttendArgs& a, int64_t f) {
 struct KvPiece {
     int h, c, t0, t1;
     bool from_start, whole;
-    int64_t next;                          // where the work after it begins
+    int64_t next, end;                     // where the work after it begins, and where that of its column tile ends
 };
 // The piece of sequence s that begins at f, in a share that ends at f1.
 template <int COLS>
@@ -152,6 +157,7 @@ __device__ __forceinline__ KvPiece kv_piece(const AttendArgs& a, const KvSeq& s,
     p.from_start = x == 0;
     p.whole = x == 0 && to == w;
     p.next = f + (to - x);
+    p.end = f + (w - x);
     return p;
 }
 // Equal shares of all work for up to `most` workgroups, none of less than `least`.
