@@ -94,6 +94,15 @@ int cf_op_attention(const uint16_t* Q, const uint16_t* K, const uint16_t* Vt, ui
 int cf_op_attention_form(const uint16_t* Q, const uint16_t* K, const uint16_t* Vt, uint16_t* O, int32_t H, int32_t nq, int32_t nk,
                          int32_t nk_pad, int32_t hd, int32_t parts, int32_t all_parts, int32_t deal, int32_t no_wait, void* scratch, uint64_t scratch_bytes,
                          void* stream);
+/* cf_kv_attention in a form of the caller's choice: 0 and 1 the kernel for few columns (query rows x query heads of a key head), 2 and 3 the one for many; 0 and 2
+ * with all work cut into equal shares and the pieces of column tiles joined, 1 and 3 with a workgroup for each column tile.  cf_plan_kv_attention is a
+ * host-only view of how a call is launched in that form, or (form -1) in the one it would take, and of the workspace that needs. */
+typedef struct cf_kv_attention_plan {
+    int32_t form, columns, workgroups, pad;       /* columns: of a column tile */
+    uint64_t workspace_bytes;
+} cf_kv_attention_plan;
+int cf_plan_kv_attention(const cf_kv_cache* cache, const cf_kv_query* queries, int32_t form, cf_kv_attention_plan* plan);
+int cf_op_kv_attention_form(const cf_kv_cache* cache, const cf_kv_query* queries, int32_t form, void* workspace, uint64_t workspace_bytes, void* stream);
 /* xn = LayerNorm(x) * (1 + scale) + shift, bf16 out. */
 int cf_op_ln_modulate(const float* x, const float* shift, const float* scale, uint16_t* xn,
                       int32_t rows, int32_t d, void* stream);

@@ -111,6 +111,10 @@ class cf_kv_query(C.Structure):
                [("scale", C.c_float), ("reserved", C.c_int32)]
 
 
+class cf_kv_attention_plan(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("form", "columns", "workgroups", "pad")] + [("workspace_bytes", C.c_uint64)]
+
+
 #: what include/chunkflow.h declares: the block path's contract
 CORE_EXPORTS = ["cf_create", "cf_destroy", "cf_last_error", "cf_blob_bytes", "cf_n_chunks", "cf_blob_layout",
                 "cf_set_block_kinds", "cf_block_kind_of", "cf_blob_bytes_of", "cf_n_chunks_of", "cf_blob_layout_of",
@@ -122,7 +126,7 @@ CORE_EXPORTS = ["cf_create", "cf_destroy", "cf_last_error", "cf_blob_bytes", "cf
                 "cf_rope_plan", "cf_rope_tables", "cf_rope_apply", "cf_kv_append", "cf_kv_attention", "cf_kv_attention_workspace"]
 #: what include/chunkflow_diag.h declares: single-kernel hooks, planner views, the matrix-core rate probe
 DIAG_EXPORTS = ["cf_plan_attention", "cf_plan_block_attention", "cf_plan_linear", "cf_plan_block_linear", "cf_plan_block_meet", "cf_plan_block_fetch", "cf_op_linear", "cf_op_linear_residual", "cf_op_linear_residual_form",
-                "cf_op_attention", "cf_op_attention_form", "cf_op_ln_modulate", "cf_op_modvec", "cf_op_mfma_rate", "cf_op_mix_rate"]
+                "cf_op_attention", "cf_op_attention_form", "cf_plan_kv_attention", "cf_op_kv_attention_form", "cf_op_ln_modulate", "cf_op_modvec", "cf_op_mfma_rate", "cf_op_mix_rate"]
 EXPORTS = CORE_EXPORTS + DIAG_EXPORTS
 
 _lib = None
@@ -195,6 +199,8 @@ def lib() -> C.CDLL:
         _lib.cf_kv_append.argtypes = [C.POINTER(cf_kv_cache), C.POINTER(cf_kv_new), C.c_void_p]
         _lib.cf_kv_attention.argtypes = [C.POINTER(cf_kv_cache), C.POINTER(cf_kv_query), C.c_void_p, C.c_uint64, C.c_void_p]
         _lib.cf_kv_attention_workspace.argtypes = [C.POINTER(cf_kv_cache), C.POINTER(cf_kv_query), C.POINTER(C.c_uint64)]
+        _lib.cf_plan_kv_attention.argtypes = [C.POINTER(cf_kv_cache), C.POINTER(cf_kv_query), C.c_int32, C.POINTER(cf_kv_attention_plan)]
+        _lib.cf_op_kv_attention_form.argtypes = [C.POINTER(cf_kv_cache), C.POINTER(cf_kv_query), C.c_int32, C.c_void_p, C.c_uint64, C.c_void_p]
         _lib.cf_op_checksum.argtypes = [C.c_void_p, C.c_uint64, C.c_uint64, C.c_void_p, C.c_void_p]
         _lib.cf_op_checksum_noalloc.argtypes = [C.c_void_p, C.c_uint64, C.c_uint64, C.c_void_p, C.c_void_p]
     return _lib
@@ -665,9 +671,7 @@ def cf_kv_attention_workspace(cache: KVCache, q, max_q: int = 0) -> int:
     return out.value
 
 
-def cf_kv_attention(cache: KVCache, q, o, cu, lens, causal: bool = False, scale: Optional[float] = None, max_q: int = 0, workspace=None, stream=None) -> None:
-    """o = softmax(scale q K^T) V for rows cu[b] .. cu[b+1] of q [tokens, heads, head_dim] (bf16) over the first lens[b] tokens of sequence b; scale: 1 / sqrt(head_dim)
-    if not given.  workspace: a dense tensor of cf_kv_attention_workspace bytes."""
+def _kv_queries(cache: KVCache, q, o, cu, lens, causal, scale, max_q, workspace) -> cf_kv_query:
     n = q.shape[0]
     if q.dim() != 3 or q.shape[2] != cache.head_dim or o.shape != q.shape:
         raise ChunkflowError(CF_ERR_ARG, f"kv_attention: q {tuple(q.shape)} and o {tuple(o.shape)}, expected [tokens, heads, {cache.head_dim}]")
@@ -675,7 +679,27 @@ def cf_kv_attention(cache: KVCache, q, o, cu, lens, causal: bool = False, scale:
     _refuse(q.stride(2) != 1 or o.stride(2) != 1, "kv_attention: the last dimension is not dense")
     _refuse(q.device != cache.device or o.device != cache.device or (workspace is not None and workspace.device != cache.device), "kv_attention: tensors on several devices")
     _refuse(workspace is not None and not workspace.is_contiguous(), "kv_attention: the workspace is not dense")
-    x = cf_kv_query(q.data_ptr(), o.data_ptr(), *_strides(q), *_strides(o), *_batch(cache, "kv_attention: cu, lens", cu, lens), n, q.shape[1], max_q, int(causal),
-                    cache.head_dim ** -0.5 if scale is None else scale, 0)
+    return cf_kv_query(q.data_ptr(), o.data_ptr(), *_strides(q), *_strides(o), *_batch(cache, "kv_attention: cu, lens", cu, lens), n, q.shape[1], max_q, int(causal),
+                       cache.head_dim ** -0.5 if scale is None else scale, 0)
+
+
+def cf_kv_attention(cache: KVCache, q, o, cu, lens, causal: bool = False, scale: Optional[float] = None, max_q: int = 0, workspace=None, stream=None) -> None:
+    """o = softmax(scale q K^T) V for rows cu[b] .. cu[b+1] of q [tokens, heads, head_dim] (bf16) over the first lens[b] tokens of sequence b; scale: 1 / sqrt(head_dim)
+    if not given.  workspace: a dense tensor of cf_kv_attention_workspace bytes."""
+    x = _kv_queries(cache, q, o, cu, lens, causal, scale, max_q, workspace)
     _launch(lib().cf_kv_attention, "kv_attention", cache.device, stream, cache.ref, C.byref(x), _ptr(workspace),
+            0 if workspace is None else workspace.numel() * workspace.element_size())
+
+
+def cf_plan_kv_attention(cache: KVCache, q, max_q: int = 0, form: int = -1) -> cf_kv_attention_plan:
+    """How cf_kv_attention (form -1) or cf_op_kv_attention_form launches queries of q's shape (host arithmetic only)."""
+    out, x = cf_kv_attention_plan(), cf_kv_query(n_tokens=q.shape[0], heads=q.shape[1], max_q=max_q)
+    _check(lib().cf_plan_kv_attention(cache.ref, C.byref(x), form, C.byref(out)))
+    return out
+
+
+def cf_op_kv_attention_form(cache: KVCache, q, o, cu, lens, form: int, causal: bool = False, scale: Optional[float] = None, max_q: int = 0, workspace=None, stream=None) -> None:
+    """cf_kv_attention in a form of the caller's choice; workspace: of cf_plan_kv_attention's bytes for it."""
+    x = _kv_queries(cache, q, o, cu, lens, causal, scale, max_q, workspace)
+    _launch(lib().cf_op_kv_attention_form, "op_kv_attention_form", cache.device, stream, cache.ref, C.byref(x), form, _ptr(workspace),
             0 if workspace is None else workspace.numel() * workspace.element_size())

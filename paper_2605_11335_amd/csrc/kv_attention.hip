@@ -5,6 +5,7 @@
 #include <chrono>
 #include <cmath>
 
+#include "../../include/chunkflow_diag.h"
 #include "context.h"
 #include "kv_tile.h"
 
@@ -803,25 +804,35 @@ bool many_whole(int64_t units, int64_t tiles) {
     return rounds * one <= (double)units * one / MANY_WGS + 25.0;
 }
 
+// Which kernel, by estimates of both (us; us per key tile of a column tile of 32 or 256 columns, all CUs at work, `fill` of the 256 taken).  32 / 8 heads,
+// few / many: 1 sequence of 8192 tokens, 64 queries 31 / 42; 8 of 8192, 12 queries each 55 / 56, 24 76 / 56, 64 171 / 87; 32 of 1024, 16 queries 29 / 31,
+// 24 43 / 32; 32 of 8192, 8 queries 98 / 147, 16 166 / 156, 64 633 / 269.
+bool many_columns(double few_tiles, double many_tiles, double fill) {
+    return 10.0 + 2.4e-3 * few_tiles > std::max(32.0, 14.0 + 1e-3 * (3.4 + 4.2 * fill) * many_tiles);
+}
+
 struct AttendPlan {
+    bool many;                         // kernel with 32 * MANY_WAVES columns per workgroup
     bool whole;                        // a workgroup per column tile
-    bool many;                         // kernel with MANY_WAVES * 32 columns per workgroup
     int cols, wgs;
-    int64_t units;                     // column tiles of all sequences and key heads, at most
     uint64_t ml_offset, cuts_offset, sent_offset, bytes;         // of the workspace
 };
 constexpr int MANY_WAVES = 8;
-const char* attend_plan(const cf_kv_cache* c, const cf_kv_query* x, AttendPlan* p) {
-    const int64_t times = x->heads / c->heads, all = (int64_t)x->n_tokens * times, most = (x->max_q && x->max_q < x->n_tokens ? x->max_q : x->n_tokens) * times;
+const char* attend_plan(const cf_kv_cache* c, const cf_kv_query* x, int form, AttendPlan* p) {
+    const int64_t times = x->heads / c->heads, all = (int64_t)x->n_tokens * times, seqs = std::min(c->n_seqs, x->n_tokens);
+    const int64_t most = (x->max_q && x->max_q < x->n_tokens ? x->max_q : x->n_tokens) * times;
     if (all > 0x7fffffff - 4096) return "too many queries";
-    p->many = most > 32;
-    p->cols = p->many ? 32 * MANY_WAVES : 32;
-    p->wgs = p->many ? MANY_WGS : FEW_WGS;
-    p->units = (all / p->cols + std::min(c->n_seqs, x->n_tokens)) * c->heads;
-    if (p->units > 0x7fffffff) return "too many queries";
-    const int64_t tiles = ((int64_t)c->table_width * c->page_tokens + KV_TILE - 1) / KV_TILE;
-    p->whole = p->many ? many_whole(p->units, tiles) : few_whole(p->units, tiles);
-    if (p->whole) p->wgs = (int)p->units;
+    // column tiles of all sequences and key heads: never more than from_all; as many as from_most if max_q is right
+    auto from_all = [&](int64_t cols) { return (all / cols + seqs) * c->heads; };
+    auto units = [&](int64_t cols) { return std::min(from_all(cols), (most + cols - 1) / cols * seqs * c->heads); };
+    const int64_t tiles = ((int64_t)c->table_width * c->page_tokens + KV_TILE - 1) / KV_TILE, wide = 32 * MANY_WAVES;
+    p->many = many_columns((double)units(32) * tiles, (double)units(wide) * tiles, (double)(all * c->heads) / (double)std::max<int64_t>(1, units(wide) * wide));
+    if (form >= 0) p->many = form >= 2;
+    p->cols = p->many ? (int)wide : 32;
+    if (from_all(p->cols) > 0x7fffffff) return "too many queries";
+    p->whole = p->many ? many_whole(units(wide), tiles) : few_whole(units(32), tiles);
+    if (form >= 0) p->whole = form & 1;
+    p->wgs = p->whole ? (int)from_all(p->cols) : p->many ? MANY_WGS : FEW_WGS;         // (a workgroup without work ends at once)
     const uint64_t slots = p->whole ? 0 : 2ull * p->wgs * p->cols;
     p->ml_offset = slots * c->head_dim * 4;
     p->cuts_offset = p->ml_offset + slots * 2 * 4;
@@ -854,26 +865,20 @@ void launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
 
 }  // namespace
 
-extern "C" int cf_kv_attention_workspace(const cf_kv_cache* cache, const cf_kv_query* x, uint64_t* bytes) {
-    if (const char* bad = kv_bad(cache)) return cf_fail(nullptr, CF_ERR_ARG, "kv_attention_workspace: %s", bad);
-    if (const char* bad = query_bad(cache, x)) return cf_fail(nullptr, CF_ERR_ARG, "kv_attention_workspace: %s", bad);
-    if (!bytes) return cf_fail(nullptr, CF_ERR_ARG, "kv_attention_workspace: null result");
-    AttendPlan p;
-    if (const char* bad = attend_plan(cache, x, &p)) return cf_fail(nullptr, CF_ERR_ARG, "kv_attention_workspace: %s", bad);
-    *bytes = p.bytes;
-    return CF_OK;
-}
-
-extern "C" int cf_kv_attention(const cf_kv_cache* cache, const cf_kv_query* x, void* workspace, uint64_t workspace_bytes, void* stream) {
-    if (const char* bad = kv_bad(cache)) return cf_fail(nullptr, CF_ERR_ARG, "kv_attention: %s", bad);
-    if (const char* bad = query_bad(cache, x)) return cf_fail(nullptr, CF_ERR_ARG, "kv_attention: %s", bad);
-    if (!(x->scale > 0.0f) || !std::isfinite(x->scale)) return cf_fail(nullptr, CF_ERR_ARG, "kv_attention: the scale must be positive and finite");
+static int attend(const char* name, const cf_kv_cache* cache, const cf_kv_query* x, int form, void* workspace, uint64_t workspace_bytes, void* stream) {
+    if (const char* bad = kv_bad(cache)) return cf_fail(nullptr, CF_ERR_ARG, "%s: %s", name, bad);
+    if (const char* bad = query_bad(cache, x)) return cf_fail(nullptr, CF_ERR_ARG, "%s: %s", name, bad);
+    if (!(x->scale > 0.0f) || !std::isfinite(x->scale)) return cf_fail(nullptr, CF_ERR_ARG, "%s: the scale must be positive and finite", name);
     if (x->n_tokens == 0 || cache->n_seqs == 0) return CF_OK;
-    if (!x->q || !x->o || !x->cu || !x->lens) return cf_fail(nullptr, CF_ERR_ARG, "kv_attention: null operand");
+    if (!x->q || !x->o || !x->cu || !x->lens) return cf_fail(nullptr, CF_ERR_ARG, "%s: null operand", name);
     if (((uintptr_t)x->q | (uintptr_t)x->o) % 16 || ((uintptr_t)x->cu | (uintptr_t)x->lens) % 4)
-        return cf_fail(nullptr, CF_ERR_ARG, "kv_attention: q and o must be 16-byte aligned, offsets and lengths 4");
+        return cf_fail(nullptr, CF_ERR_ARG, "%s: q and o must be 16-byte aligned, offsets and lengths 4", name);
     for (const int64_t st : {x->q_row, x->q_head, x->o_row, x->o_head})
-        if (st < 0 || st > (int64_t)1 << 40 || st % 8) return cf_fail(nullptr, CF_ERR_ARG, "kv_attention: strides must be multiples of 16 bytes and not negative");
+        if (st < 0 || st > (int64_t)1 << 40 || st % 8) return cf_fail(nullptr, CF_ERR_ARG, "%s: strides must be multiples of 16 bytes and not negative", name);
+    AttendPlan p;
+    if (const char* bad = attend_plan(cache, x, form, &p)) return cf_fail(nullptr, CF_ERR_ARG, "%s: %s", name, bad);
+    if (p.bytes && (!workspace || (uintptr_t)workspace % 256 || workspace_bytes < p.bytes))
+        return cf_fail(nullptr, CF_ERR_ARG, "%s: a workspace of %llu bytes, 256-byte aligned, is needed", name, (unsigned long long)p.bytes);
     AttendArgs a = {};
     a.c = kv_view(*cache);
     a.q = (const bf16*)x->q; a.o = (bf16*)x->o;
@@ -881,21 +886,50 @@ extern "C" int cf_kv_attention(const cf_kv_cache* cache, const cf_kv_query* x, v
     a.cu = x->cu; a.lens = x->lens;
     a.n_tokens = x->n_tokens; a.heads = x->heads; a.times = x->heads / cache->heads;
     a.causal = x->causal != 0;
-    a.c2 = x->scale * 1.4426950408889634f;
-    AttendPlan p;
-    if (const char* bad = attend_plan(cache, x, &p)) return cf_fail(nullptr, CF_ERR_ARG, "kv_attention: %s", bad);
-    if (p.bytes && (!workspace || (uintptr_t)workspace % 256 || workspace_bytes < p.bytes))
-        return cf_fail(nullptr, CF_ERR_ARG, "kv_attention: a workspace of %llu bytes, 256-byte aligned, is needed", (unsigned long long)p.bytes);
     a.whole = p.whole;
-    a.part_o = (float*)workspace;
-    a.part_ml = (float*)((char*)workspace + p.ml_offset);
-    a.cuts = (KvCut*)((char*)workspace + p.cuts_offset);
-    a.sent = (unsigned long long*)((char*)workspace + p.sent_offset);
-    a.joined = (uint32_t*)(a.sent + p.wgs * MANY_WAVES);
-    a.epoch = next_epoch();
-    hipStream_t s = (hipStream_t)stream;
-    if (cache->head_dim == 128) launch<128>(a, p, s);
-    else launch<64>(a, p, s);
+    a.c2 = x->scale * 1.4426950408889634f;
+    if (!p.whole) {
+        a.part_o = (float*)workspace;
+        a.part_ml = (float*)((char*)workspace + p.ml_offset);
+        a.cuts = (KvCut*)((char*)workspace + p.cuts_offset);
+        a.sent = (unsigned long long*)((char*)workspace + p.sent_offset);
+        a.joined = (uint32_t*)(a.sent + p.wgs * MANY_WAVES);
+        a.epoch = next_epoch();
+    }
+    if (cache->head_dim == 128) launch<128>(a, p, (hipStream_t)stream);
+    else launch<64>(a, p, (hipStream_t)stream);
     const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? CF_OK : cf_fail(nullptr, CF_ERR_HIP, "kv_attention launch: %s", hipGetErrorString(e));
+    return e == hipSuccess ? CF_OK : cf_fail(nullptr, CF_ERR_HIP, "%s launch: %s", name, hipGetErrorString(e));
+}
+
+static int attend_view(const char* name, const cf_kv_cache* cache, const cf_kv_query* x, int form, AttendPlan* p) {
+    if (const char* bad = kv_bad(cache)) return cf_fail(nullptr, CF_ERR_ARG, "%s: %s", name, bad);
+    if (const char* bad = query_bad(cache, x)) return cf_fail(nullptr, CF_ERR_ARG, "%s: %s", name, bad);
+    if (const char* bad = attend_plan(cache, x, form, p)) return cf_fail(nullptr, CF_ERR_ARG, "%s: %s", name, bad);
+    return CF_OK;
+}
+
+extern "C" int cf_kv_attention_workspace(const cf_kv_cache* cache, const cf_kv_query* x, uint64_t* bytes) {
+    if (!bytes) return cf_fail(nullptr, CF_ERR_ARG, "kv_attention_workspace: null result");
+    AttendPlan p;
+    CF_TRY(attend_view("kv_attention_workspace", cache, x, -1, &p));
+    *bytes = p.bytes;
+    return CF_OK;
+}
+
+extern "C" int cf_plan_kv_attention(const cf_kv_cache* cache, const cf_kv_query* x, int32_t form, cf_kv_attention_plan* plan) {
+    if (!plan || form < -1 || form > 3) return cf_fail(nullptr, CF_ERR_ARG, "plan_kv_attention: form is -1 to 3, the result not NULL");
+    AttendPlan p;
+    CF_TRY(attend_view("plan_kv_attention", cache, x, form, &p));
+    *plan = {p.many ? 2 + p.whole : 0 + p.whole, p.cols, p.wgs, 0, p.bytes};
+    return CF_OK;
+}
+
+extern "C" int cf_kv_attention(const cf_kv_cache* cache, const cf_kv_query* x, void* workspace, uint64_t workspace_bytes, void* stream) {
+    return attend("kv_attention", cache, x, -1, workspace, workspace_bytes, stream);
+}
+
+extern "C" int cf_op_kv_attention_form(const cf_kv_cache* cache, const cf_kv_query* x, int32_t form, void* workspace, uint64_t workspace_bytes, void* stream) {
+    if (form < 0 || form > 3) return cf_fail(nullptr, CF_ERR_ARG, "op_kv_attention_form: form is 0 to 3");
+    return attend("op_kv_attention_form", cache, x, form, workspace, workspace_bytes, stream);
 }

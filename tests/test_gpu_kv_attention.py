@@ -10,7 +10,10 @@ from tests.util import bf16_round, dev_bits
 pytestmark = pytest.mark.gpu
 
 
-def run(cache, q_bits, cu, lens, causal=False, scale=None, max_q=0, dev=None, stream=None, strided=False):
+FORMS = (-1, 0, 1, 2, 3)         # the planner's, few columns cut and whole, many cut and whole
+
+
+def run(cache, q_bits, cu, lens, causal=False, scale=None, max_q=0, dev=None, stream=None, strided=False, form=-1):
     """Output [rows, heads, hd] in 64 bits; rows of no sequence keep a mark (7)."""
     q = dev_bits(q_bits).view(torch.bfloat16)
     if strided:                                     # heads outside rows, with a gap behind every head
@@ -21,22 +24,31 @@ def run(cache, q_bits, cu, lens, causal=False, scale=None, max_q=0, dev=None, st
     else:
         o = torch.full_like(q, 7.0)
     dev = cache.device(B) if dev is None else dev
-    need = B.cf_kv_attention_workspace(dev, q, max_q)
+    need = B.cf_plan_kv_attention(dev, q, max_q, form).workspace_bytes
     ws = torch.full((need,), 255, dtype=torch.uint8, device=DEV)           # (NaN, should anything be read before it is written)
-    B.cf_kv_attention(dev, q, o, lens_t(cu), lens_t(lens), causal, scale, max_q, ws, stream)
+    if form < 0:
+        assert need == B.cf_kv_attention_workspace(dev, q, max_q)
+        B.cf_kv_attention(dev, q, o, lens_t(cu), lens_t(lens), causal, scale, max_q, ws, stream)
+    else:
+        B.cf_op_kv_attention_form(dev, q, o, lens_t(cu), lens_t(lens), form, causal, scale, max_q, ws, stream)
     torch.cuda.synchronize()
     return o.double().cpu().numpy()
 
 
-def check(cache, q, cu, lens, causal=False, scale=None, **kw):
+def check(cache, q, cu, lens, causal=False, scale=None, forms=FORMS, **kw):
+    """Every form against the definition; their outputs."""
     val, bits = bf16_round(q)
-    got = run(cache, bits, cu, lens, causal, scale, **kw)
     want, tol = attention(cache, val.astype(np.float64), cu, lens, causal, cache.hd ** -0.5 if scale is None else scale)
     mine = ~np.isnan(want[:, 0, 0])
-    bad = ~(np.abs(got - want) <= tol)
-    assert not bad[mine].any(), f"{bad[mine].sum()} of {bad[mine].size}, worst {np.nanmax((np.abs(got - want) - tol)[mine]):.3e} over, at {np.argwhere(bad & mine[:, None, None])[:5].tolist()}"
-    assert (got[~mine] == 7).all()
-    return got
+    dev, out = cache.device(B), []
+    for form in forms:
+        got = run(cache, bits, cu, lens, causal, scale, dev=dev, form=form, **kw)
+        bad = ~(np.abs(got - want) <= tol)
+        assert not bad[mine].any(), f"form {form}: {bad[mine].sum()} of {bad[mine].size}, worst {np.nanmax((np.abs(got - want) - tol)[mine]):.3e} over, " \
+                                    f"at {np.argwhere(bad & mine[:, None, None])[:5].tolist()}"
+        assert (got[~mine] == 7).all()
+        out.append(got)
+    return out
 
 
 def offsets(n, first=0):
@@ -83,7 +95,7 @@ def test_pages_that_are_not_there_and_pages_that_are_shared(n, hd):
     cache.table[1] = -2                                               # no page at all
     cache.table[2] = cache.table[3]
     got = check(cache, rng.normal(size=(4 * n, 4, hd)), offsets([n] * 4), [400, 400, 400, 390], n > 1)
-    assert (got[n:2 * n] == 0).all()
+    assert all((g[n:2 * n] == 0).all() for g in got)
     # more tokens than the table has room for, and a negative number of them
     check(cache, rng.normal(size=(4 * n, 4, hd)), offsets([n] * 4), [2 ** 31 - 1, 0, -5, 100000])
 
@@ -108,19 +120,21 @@ def test_codes_that_no_query_sees_are_anything(n, hd):
     cache.k[np.broadcast_to(unseen[..., None, :, None], cache.k.shape)] = 0x7f
     cache.v[np.broadcast_to(unseen[..., None, :], cache.v.shape)] = 0xff
     cache.scales[np.broadcast_to(~seen.any(-1)[:, None, :, None], cache.scales.shape)] = 255
-    assert np.array_equal(check(cache, q, cu, lens), clean)
+    for form, got, was in zip(FORMS, check(cache, q, cu, lens), clean):
+        assert np.array_equal(got, was), form
 
 
+@pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("n", [5, 90])
-def test_causal_queries_do_not_see_what_comes_after_them(hd, n):
+def test_causal_queries_do_not_see_what_comes_after_them(hd, n, form):
     """Keys and values of NaN behind query j leave the queries up to j as they are, and reach all others."""
     rng = np.random.default_rng(hd + n)
     held = n + 37
     cache = Cache(rng, 1, 2, hd, 32, held, fill="small")
     _, bits = bf16_round(rng.normal(size=(n, 4, hd)))
     cu = offsets([n])
-    clean = run(cache, bits, cu, [held], True)
+    clean = run(cache, bits, cu, [held], True, form=form)
     for which in ("k", "v"):
         for j in (0, n // 2, n - 2):
             pg, g = cache.group(0, held - n + j + 1)
@@ -130,7 +144,7 @@ def test_causal_queries_do_not_see_what_comes_after_them(hd, n):
                 cache.k[pg, 1, g, 0, slot, 3] = 0x7f
             else:
                 cache.v[pg, 1, g, 5, slot] = 0x7f
-            got = run(cache, bits, cu, [held], True)
+            got = run(cache, bits, cu, [held], True, form=form)
             assert np.array_equal(got[:, :2], clean[:, :2]) and np.array_equal(got[:j + 1], clean[:j + 1]), (which, j)
             hit = got[j + 1:, 2:] if which == "k" else got[j + 1:, 2:, 5]
             assert np.isnan(hit).all(), (which, j)
@@ -169,8 +183,9 @@ def test_powers_of_two_from_end_to_end_and_a_query_that_is_nan():
     q = rng.normal(size=(6, 4, 128))
     check(cache, q, offsets([5, 1]), [200, 77])
     q[2, 1] = np.nan
-    got = run(cache, bf16_round(np.where(np.isnan(q), 0, q))[1] | np.where(np.isnan(q), 0x7fc0, 0).astype(np.uint16), offsets([5, 1]), [200, 77])
-    assert np.isnan(got[2, 1]).all() and np.isfinite(np.delete(got.reshape(24, 128), 9, 0)).all()
+    for form in FORMS:
+        got = run(cache, bf16_round(np.where(np.isnan(q), 0, q))[1] | np.where(np.isnan(q), 0x7fc0, 0).astype(np.uint16), offsets([5, 1]), [200, 77], form=form)
+        assert np.isnan(got[2, 1]).all() and np.isfinite(np.delete(got.reshape(24, 128), 9, 0)).all()
 
 
 def test_scale_and_every_power_of_the_format():
@@ -182,10 +197,11 @@ def test_scale_and_every_power_of_the_format():
         cache.scales[cache.table[b, 0], 0, 0, 1] = b + 1
     cache.v[:, 0, 0, :, 0] = np.where(cache.v[:, 0, 0, :, 0] & 0x78, cache.v[:, 0, 0, :, 0], 0x38)        # normal codes
     _, bits = bf16_round(rng.normal(size=(seqs, 1, 64)))
-    got = run(cache, bits, offsets([1] * seqs), [1] * seqs, scale=3.5)
     want = np.stack([cache.held(b, 1)[1][0, 0] for b in range(seqs)])
     inside = (np.abs(want) >= 2.0 ** -126) & (np.abs(want) < 2.0 ** 127)
-    assert np.array_equal(got[:, 0][inside], want[inside]) and (np.abs(got[:, 0] - want)[~inside & (np.abs(want) < 2.0 ** -126)] <= 2.0 ** -126).all()
+    for form in FORMS:
+        got = run(cache, bits, offsets([1] * seqs), [1] * seqs, scale=3.5, form=form)
+        assert np.array_equal(got[:, 0][inside], want[inside]) and (np.abs(got[:, 0] - want)[~inside & (np.abs(want) < 2.0 ** -126)] <= 2.0 ** -126).all()
 
 
 @pytest.mark.parametrize("n,held", [(1, 20001), (3, 9000), (1, 130001)])
@@ -195,8 +211,9 @@ def test_long_caches(n, held):
     check(cache, rng.normal(size=(2 * n, 4, 128)), offsets([n, n]), [held, held // 3], n > 1, max_q=n)
 
 
+@pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("n", [1, 64])
-def test_a_cache_past_4_gib(n):
+def test_a_cache_past_4_gib(n, form):
     """Pages whose codes lie behind 2^32 bytes, among them the last."""
     heads, hd, page, pages = 8, 128, 128, 45000                     # 5.9 GB of K and of V
     k = torch.zeros(pages, heads, page // 16, hd // 16, 16, 16, dtype=torch.uint8, device=DEV)
@@ -210,37 +227,60 @@ def test_a_cache_past_4_gib(n):
         k[p], v[p], scales[p] = (torch.from_numpy(x[src]).to(DEV) for x in (small.k, small.v, small.scales))
     big = B.make_kv_cache(k, v, scales, torch.tensor([at], dtype=torch.int32, device=DEV))
     _, bits = bf16_round(rng.normal(size=(n, 8, hd)))
-    want, got = run(small, bits, offsets([n]), [600], max_q=n), run(small, bits, offsets([n]), [600], max_q=n, dev=big)
+    want, got = run(small, bits, offsets([n]), [600], max_q=n, form=form), run(small, bits, offsets([n]), [600], max_q=n, dev=big, form=form)
     assert np.array_equal(want, got)
 
 
+@pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("n", [1, 60])
-def test_replays_of_a_captured_call_on_other_lengths(n):
+def test_replays_of_a_captured_call_on_other_lengths(n, form):
+    """... and of two calls that share a workspace, with other calls in it between the replays."""
     rng = np.random.default_rng(n)
     cache = Cache(rng, 3, 2, 128, 32, 3000, fill="small")
     dev = cache.device(B)
     _, bits = bf16_round(rng.normal(size=(3 * n, 8, 128)))
     q = dev_bits(bits).view(torch.bfloat16)
-    cu, lens, o = lens_t(offsets([n] * 3)), lens_t([n] * 3), torch.zeros_like(q)
-    ws = torch.empty(B.cf_kv_attention_workspace(dev, q, n), dtype=torch.uint8, device=DEV)
+    cu, lens, o, o2 = lens_t(offsets([n] * 3)), lens_t([n] * 3), torch.zeros_like(q), torch.zeros_like(q)
+    ws = torch.empty(max(B.cf_plan_kv_attention(dev, q, n, f).workspace_bytes for f in FORMS), dtype=torch.uint8, device=DEV)
+
+    def call(form, o, causal):
+        if form < 0:
+            B.cf_kv_attention(dev, q, o, cu, lens, causal, None, n, ws)
+        else:
+            B.cf_op_kv_attention_form(dev, q, o, cu, lens, form, causal, None, n, ws)
+
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        B.cf_kv_attention(dev, q, o, cu, lens, True, None, n, ws)
-    for held in ([n, n + 1, 2 * n], [3000, 1, 700], [0, 64, 2999], [3000, 3000, 3000]):
+        call(form, o, True)
+        call(2, o2, False)
+    for held in ([n, n + 1, 2 * n], [3000, 1, 700], [0, 64, 2999], [3000, 3000, 3000], [3000, 3000, 3000]):
         lens.copy_(lens_t(held))
         o.fill_(3.0)
         graph.replay()
         torch.cuda.synchronize()
-        assert np.array_equal(o.double().cpu().numpy(), run(cache, bits, offsets([n] * 3), held, True, max_q=n, dev=dev)), held
+        assert np.array_equal(o.double().cpu().numpy(), run(cache, bits, offsets([n] * 3), held, True, max_q=n, dev=dev, form=form)), held
+        assert np.array_equal(o2.double().cpu().numpy(), run(cache, bits, offsets([n] * 3), held, False, max_q=n, dev=dev, form=2)), held
+        call((form + 1) % 4, o, False)
 
 
-@pytest.mark.parametrize("n", [1, 60])
-def test_the_same_call_gives_the_same_bits(n):
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("n,heads", [(1, 6), (60, 6), (700, 12)])
+def test_the_same_call_gives_the_same_bits(n, heads, form):
+    """Whichever workgroup joins the pieces of a column tile, and when."""
     rng = np.random.default_rng(n)
     cache = Cache(rng, 2, 3, 128, 64, 5000, fill="small")
     dev = cache.device(B)
-    _, bits = bf16_round(rng.normal(size=(2 * n, 6, 128)))
-    first = run(cache, bits, offsets([n] * 2), [5000, 4321], dev=dev, max_q=n)
+    _, bits = bf16_round(rng.normal(size=(2 * n, heads, 128)))
+    first = run(cache, bits, offsets([n] * 2), [5000, 4321], dev=dev, max_q=n, form=form)
     side = torch.cuda.Stream()
-    for stream in (None, side, None):
-        assert np.array_equal(first, run(cache, bits, offsets([n] * 2), [5000, 4321], dev=dev, max_q=n, stream=stream))
+    for stream in (None, side, None, None):
+        assert np.array_equal(first, run(cache, bits, offsets([n] * 2), [5000, 4321], dev=dev, max_q=n, stream=stream, form=form))
+
+
+def test_the_planner_takes_every_form():
+    """A token over a long cache, over a short one, a few thousand queries over a clip, a few hundred over one text for every head."""
+    def form(queries, heads, kv_heads, seqs, capacity):
+        z = lambda *s: torch.zeros(*s, dtype=torch.uint8, device=DEV)       # noqa: E731
+        cache = B.make_kv_cache(z(1, kv_heads, 4, 8, 16, 16), z(1, kv_heads, 4, 128, 16), z(1, kv_heads, 4, 2), torch.zeros(seqs, capacity // 64, dtype=torch.int32, device=DEV))
+        return B.cf_plan_kv_attention(cache, torch.empty(queries, heads, 128, dtype=torch.bfloat16, device=DEV)).form
+    assert [form(1, 12, 12, 1, 131072), form(16, 8, 8, 16, 512), form(3520, 12, 12, 1, 27264), form(2560, 24, 24, 1, 2048)] == [0, 1, 2, 3]
