@@ -51,15 +51,16 @@ __device__ __forceinline__ uint32_t moved(uint32_t w, int up) {
     return (uint32_t)r;
 }
 // A pair of dims as it lies in memory: a word of two bf16, or two floats.
+typedef float floatx2 __attribute__((ext_vector_type(2)));
 template <class T>
-using Pair = std::conditional_t<sizeof(T) == 2, uint32_t, float2>;
+using Pair = std::conditional_t<sizeof(T) == 2, uint32_t, floatx2>;
 __device__ __forceinline__ void unpack(uint32_t w, float& a, float& b) {
     a = __uint_as_float(w << 16);
     b = __uint_as_float(w & 0xffff0000u);
 }
-__device__ __forceinline__ void unpack(float2 w, float& a, float& b) {
-    a = w.x;
-    b = w.y;
+__device__ __forceinline__ void unpack(floatx2 w, float& a, float& b) {
+    a = w[0];
+    b = w[1];
 }
 
 // A wave has one group at a time, all of it: lane = a pair of dims, for 16 tokens (8 with 64-wide heads, whose other half of the lanes has the other 8).
@@ -106,7 +107,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
             const T* p = at + s0 * stride;                                     // (one pointer from row to row: 16 of them would be kept in registers)
             asm volatile("" : "+v"(p));
 #pragma unroll
-            for (int t = 0; t < TPL; ++t) raw[t] = *(const Pair<T>*)(p + t * stride);
+            for (int t = 0; t < TPL; ++t) raw[t] = __builtin_nontemporal_load((const Pair<T>*)(p + t * stride));
         } else {                                                               // slots without a new token repeat one that has
 #pragma unroll
             for (int t = 0; t < TPL; ++t) raw[t] = *(const Pair<T>*)(at + kv_clamped(s0 + t, lo, hi - 1) * stride);

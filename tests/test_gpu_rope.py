@@ -189,3 +189,19 @@ def test_a_block_over_positions_on_three_axes():
             run.rope_tables(B.cf_rope_plan(128, [64]), torch.zeros(5, 1, dtype=torch.int32, device=DEV))
     finally:
         run.close()
+
+
+@pytest.mark.parametrize("dtype,hd,heads", [(torch.bfloat16, 64, 17), (torch.bfloat16, 128, 8), (torch.float32, 64, 5), (torch.float32, 128, 3)])
+def test_operands_that_caches_do_not_hold(dtype, hd, heads):
+    """Outputs of more than 64 MiB, which go past the caches: the bits of the same rows a few at a time."""
+    n = (68 << 20) // (heads * hd * dtype.itemsize) + 5
+    plan = B.cf_rope_plan(hd, [hd // 4, hd // 8])
+    p = torch.randint(-1000, 1000000, (n, 2), dtype=torch.int32, device=DEV)
+    x = torch.randn(n, heads, hd, device=DEV).to(dtype)
+    whole, parts = torch.empty_like(x), torch.empty_like(x)
+    B.cf_rope_apply(plan, p, x, whole)
+    for i in range(0, n, n // 3 + 1):
+        B.cf_rope_apply(plan, p[i:i + n // 3 + 1], x[i:i + n // 3 + 1], parts[i:i + n // 3 + 1])
+    assert torch.equal(whole, parts)
+    B.cf_rope_apply(plan, p, x, x)
+    assert torch.equal(whole, x)
