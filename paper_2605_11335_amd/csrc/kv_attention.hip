@@ -20,7 +20,8 @@ constexpr int FEW_WAVES = 4, FEW_LEAST = 5 * KV_TILE;           // FEW_LEAST: we
 
 // One column tile of 32 over key tiles [t0, t1), of which each wave takes every FEW_WAVES-th: its own result.  Tiles that every column sees whole
 // come first, one after the other without a break in the loads; then those with an end, a hole in the page table or a power that is none, if there are any.
-template <int HD>
+// FAR: codes go past the caches, where each is read once and there are more of them than the caches hold.
+template <int HD, bool FAR>
 __device__ __forceinline__ void few_sweep(const AttendArgs& a, const KvSeq& q, int h, int c, int t0, int t1, const bf16x8 (*sq)[64], KvState<HD>& st) {
     constexpr int KJ = HD / 32, DT = HD / 32, GB = 16 * HD, STEP = FEW_WAVES;
     const int lane = threadIdx.x & 63, lj = lane & 31, lg = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -47,6 +48,10 @@ __device__ __forceinline__ void few_sweep(const AttendArgs& a, const KvSeq& q, i
     const int slot = (lj & 3) + 4 * (lj >> 3), kg = (lj >> 2) & 1;
     uint32x4 kq[2][KJ], vq[2][DT];
     uint32_t ksc[2], vsc[2];
+    auto codes = [](const uint8_t* p) __attribute__((always_inline)) {
+        if constexpr (FAR) return __builtin_nontemporal_load((const uint32x4*)p);
+        else return *(const uint32x4*)p;
+    };
     auto load_k = [&](int g, uint32_t p, int nth) __attribute__((always_inline)) {
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
@@ -54,7 +59,7 @@ __device__ __forceinline__ void few_sweep(const AttendArgs& a, const KvSeq& q, i
             ksc[mt] = __shfl(p, from) & 255u;
             const uint8_t* const at = a.c.k + (int64_t)max(__shfl(g, from), 0) * GB + lg * 256 + slot * 16;
 #pragma unroll
-            for (int j = 0; j < KJ; ++j) kq[mt][j] = *(const uint32x4*)(at + j * 512);
+            for (int j = 0; j < KJ; ++j) kq[mt][j] = codes(at + j * 512);
         }
     };
     auto load_v = [&](int g, uint32_t p, int nth) __attribute__((always_inline)) {
@@ -64,7 +69,7 @@ __device__ __forceinline__ void few_sweep(const AttendArgs& a, const KvSeq& q, i
             vsc[s] = __shfl(p, from) >> 8;
             const uint8_t* const at = a.c.v + (int64_t)max(__shfl(g, from), 0) * GB + lj * 16;
 #pragma unroll
-            for (int d = 0; d < DT; ++d) vq[s][d] = *(const uint32x4*)(at + d * 512);
+            for (int d = 0; d < DT; ++d) vq[s][d] = codes(at + d * 512);
         }
     };
     floatx16 s[2];
@@ -211,7 +216,7 @@ __device__ __forceinline__ void few_sweep(const AttendArgs& a, const KvSeq& q, i
     }
 }
 
-template <int HD>
+template <int HD, bool FAR>
 __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attend_few_kernel(AttendArgs a) {
     constexpr int DT = HD / 32;
     __shared__ __attribute__((aligned(16))) float so[FEW_WAVES][DT * 4][64][4];
@@ -235,7 +240,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attend_few_kernel(Attend
                 sq[k][lane] = *(const bf16x8*)(a.q + (int64_t)col.row * a.q_row + (int64_t)col.head * a.q_head + 32 * (k >> 1) + 16 * lg + 8 * (k & 1));
             __syncthreads();
             KvState<HD> st;
-            few_sweep<HD>(a, q, h, c, p.t0, p.t1, sq, st);
+            few_sweep<HD, FAR>(a, q, h, c, p.t0, p.t1, sq, st);
             const float l = st.l + __shfl_xor(st.l, 32);
 #pragma unroll
             for (int i = 0; i < DT * 4; ++i)
@@ -623,7 +628,8 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
                 joined = true;
             }
             if (cols > 0 && (p.whole || joined)) {
-                // rows of 2 head_dim bytes, 16 per lane: stored by dims of a lane, an instruction would touch 32 rows (13640 queries x 24 heads: 60 us of stores)
+                // rows of 2 head_dim bytes, 16 per lane: stored by dims of a lane, an instruction would touch 32 rows.  Past the caches, which have the keys and
+                // values that all workgroups share (13640 queries x 512 tokens x 24 heads: 115.8 us, 119.8 through them).
                 const float inv = kv_inverse(l);
                 const int ln = anew(lane), col_l = ln & 31, half = ln >> 5;
                 char* const rows = (char*)&sh.k + wave * (64 * HD);            // where tiles were: k and v are as large as the outputs
@@ -642,7 +648,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
                     const int r = i * (512 / HD) + ln / (HD / 8), ch = ln % (HD / 8);
                     const KvColumn to = kv_column(a, q, p.h, col0 + r);
                     const bf16x8 x = *(const bf16x8*)(rows + many_row<HD>(r, ch));
-                    if (r < cols) *(bf16x8*)(a.o + (int64_t)to.row * a.o_row + (int64_t)to.head * a.o_head + ch * 8) = x;
+                    if (r < cols) __builtin_nontemporal_store(x, (bf16x8*)(a.o + (int64_t)to.row * a.o_row + (int64_t)to.head * a.o_head + ch * 8));
                 }
                 lds_order();
             } else if (cols > 0) {
@@ -814,6 +820,7 @@ bool many_columns(double few_tiles, double many_tiles, double fill) {
 struct AttendPlan {
     bool many;                         // kernel with 32 * MANY_WAVES columns per workgroup
     bool whole;                        // a workgroup per column tile
+    bool far;                          // few columns: codes past the caches
     int cols, wgs;
     uint64_t ml_offset, cuts_offset, sent_offset, bytes;         // of the workspace
 };
@@ -832,6 +839,9 @@ const char* attend_plan(const cf_kv_cache* c, const cf_kv_query* x, int form, At
     if (from_all(p->cols) > 0x7fffffff) return "too many queries";
     p->whole = p->many ? many_whole(units(wide), tiles) : few_whole(units(32), tiles);
     if (form >= 0) p->whole = form & 1;
+    // One column tile per sequence and key head reads every code once.  32 ragged sequences of up to 8201 tokens x 8 heads 63.7 us, through the caches 72.9; one of
+    // 131001 x 12 73.6 / 83.0.  (64 MiB: twice what the L2 caches hold.)
+    p->far = !p->many && most <= 32 && seqs * tiles * c->heads > (64ll << 20) / (2 * KV_TILE * c->head_dim);
     p->wgs = p->whole ? (int)from_all(p->cols) : p->many ? MANY_WGS : FEW_WGS;         // (a workgroup without work ends at once)
     const uint64_t slots = p->whole ? 0 : 2ull * p->wgs * p->cols;
     p->ml_offset = slots * c->head_dim * 4;
@@ -858,7 +868,8 @@ void launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
         hipLaunchKernelGGL((kv_attend_many_kernel<HD, MANY_WAVES>), dim3(p.wgs), dim3(64 * MANY_WAVES), 0, s, a);
         if (!p.whole) hipLaunchKernelGGL((kv_join_kernel<HD, 32 * MANY_WAVES, 256>), dim3(p.wgs - 1, MANY_WAVES), dim3(256), 0, s, a);
     } else {
-        hipLaunchKernelGGL(kv_attend_few_kernel<HD>, dim3(p.wgs), dim3(64 * FEW_WAVES), 0, s, a);
+        if (p.far) hipLaunchKernelGGL((kv_attend_few_kernel<HD, true>), dim3(p.wgs), dim3(64 * FEW_WAVES), 0, s, a);
+        else hipLaunchKernelGGL((kv_attend_few_kernel<HD, false>), dim3(p.wgs), dim3(64 * FEW_WAVES), 0, s, a);
         if (!p.whole) hipLaunchKernelGGL((kv_join_kernel<HD, 32, 1024>), dim3(p.wgs - 1), dim3(1024), 0, s, a);
     }
 }

@@ -8,6 +8,9 @@ device-to-device copy of known size, used to calibrate hardware byte counters.
     python -m paper_2605_11335_amd.kernel_bench checksum 283183616 [iters]  # bytes (a C2 blob)
     python -m paper_2605_11335_amd.kernel_bench mfma_rate 20000 [iters]     # MFMAs on registers only
     python -m paper_2605_11335_amd.kernel_bench mix_rate 20000 [iters]      # MFMAs beside LDS reads and VALU work
+    python -m paper_2605_11335_amd.kernel_bench rope 13640x24x128 [iters]   # rows x heads x head width, q and k
+    python -m paper_2605_11335_amd.kernel_bench kv_append 20460x12x128 [iters]          # new tokens x heads x head width
+    python -m paper_2605_11335_amd.kernel_bench kv_attention 32x1x8192x32x8x128 [iters] # sequences x queries x tokens x heads x cache heads x width
 
 Timing uses events on the current stream; inputs are seeded N(0,1) activations and N(0,0.02)
 weights in bf16.  The GEMM benchmarks rotate over enough operand sets that consecutive launches
@@ -104,6 +107,39 @@ def main(argv):
             base = base or tf
             print(f"mix_rate waves/CU {waves}  LDS reads per 16 MFMAs {reads:2d}  VALU per MFMA {valu}  exp2 per MFMA {exps}: "
                   f"{ms:8.3f} ms  {tf:7.1f} TFLOP/s  ({tf / base * 100:5.1f} % of MFMAs alone)")
+    elif which == "rope":
+        n, H, hd = (int(v) for v in shape.split("x"))
+        plan, pos = B.cf_rope_plan(hd, [hd // 4, hd // 8, hd // 8]), torch.randint(0, 1000, (n, 3), dtype=torch.int32, device=DEV)
+        q, k = (torch.randn(n, H, hd, device=DEV).to(torch.bfloat16) for _ in range(2))
+        qo, ko = torch.empty_like(q), torch.empty_like(k)
+        ms = timeit(lambda: B.cf_rope_apply(plan, pos, q, qo, k, ko), iters)
+        print(f"rope {n} rows, q and k of {H} heads x {hd}: {ms * 1e3:.1f} us  {8 * n * H * hd / ms / 1e6:.1f} GB/s (read + write)")
+    elif which in ("kv_append", "kv_attention"):
+        v = [int(x) for x in shape.split("x")]
+        seqs, n, held, H, kvh, hd = (1, v[0], 0, v[1], v[1], v[2]) if which == "kv_append" else v
+        page, most = 64, max(held, n if which == "kv_append" else 1)
+        per_seq = -(-most // page)
+        cache = B.make_kv_cache(torch.empty(seqs * per_seq, kvh, page // 16, hd // 16, 16, 16, dtype=torch.uint8, device=DEV),
+                                torch.empty(seqs * per_seq, kvh, page // 16, hd, 16, dtype=torch.uint8, device=DEV),
+                                torch.empty(seqs * per_seq, kvh, page // 16, 2, dtype=torch.uint8, device=DEV),
+                                torch.randperm(seqs * per_seq, device=DEV).to(torch.int32).view(seqs, per_seq))
+        offsets = lambda k: torch.arange(seqs + 1, dtype=torch.int32, device=DEV) * k      # noqa: E731
+        full = lambda k: torch.full((seqs,), k, dtype=torch.int32, device=DEV)             # noqa: E731
+        new = n if which == "kv_append" else held
+        k_new, v_new = (torch.randn(seqs * new, kvh, hd, device=DEV).to(torch.bfloat16) for _ in range(2))
+        append = lambda: B.cf_kv_append(cache, k_new, v_new, offsets_new, none)            # noqa: E731
+        offsets_new, none = offsets(new), full(0)
+        if which == "kv_append":
+            ms = timeit(append, iters)
+            print(f"kv_append {n} tokens x {kvh} heads x {hd}: {ms * 1e3:.1f} us  {6 * n * kvh * hd / ms / 1e6:.1f} GB/s (bf16 in, codes out)")
+        else:
+            append()
+            q = torch.randn(seqs * n, H, hd, device=DEV).to(torch.bfloat16)
+            o, cu, lens = torch.empty_like(q), offsets(n), full(held)
+            ws = torch.empty(B.cf_kv_attention_workspace(cache, q, n), dtype=torch.uint8, device=DEV)
+            ms = timeit(lambda: B.cf_kv_attention(cache, q, o, cu, lens, max_q=n, workspace=ws), iters)
+            print(f"kv_attention {seqs} x {n} queries over {held} tokens, {H} / {kvh} heads x {hd}: {ms * 1e3:.1f} us  "
+                  f"{2 * seqs * held * kvh * hd / ms / 1e6:.1f} GB/s of codes  {4 * seqs * n * held * H * hd / ms / 1e9:.1f} TFLOP/s")
     else:
         raise SystemExit(__doc__)
 

@@ -204,11 +204,12 @@ def test_scale_and_every_power_of_the_format():
         assert np.array_equal(got[:, 0][inside], want[inside]) and (np.abs(got[:, 0] - want)[~inside & (np.abs(want) < 2.0 ** -126)] <= 2.0 ** -126).all()
 
 
-@pytest.mark.parametrize("n,held", [(1, 20001), (3, 9000), (1, 130001)])
-def test_long_caches(n, held):
-    rng = np.random.default_rng(held)
-    cache = Cache(rng, 2, 2, 128, 128, held, fill="small")
-    check(cache, rng.normal(size=(2 * n, 4, 128)), offsets([n, n]), [held, held // 3], n > 1, max_q=n)
+@pytest.mark.parametrize("n,held,hd,kv_heads", [(1, 20001, 128, 2), (3, 9000, 128, 2), (1, 130001, 128, 2), (1, 130001, 64, 4)])
+def test_long_caches(n, held, hd, kv_heads):
+    """(Of 130001 tokens: one query each goes past the caches.)"""
+    rng = np.random.default_rng(held + hd)
+    cache = Cache(rng, 2, kv_heads, hd, 128, held, fill="small")
+    check(cache, rng.normal(size=(2 * n, 2 * kv_heads, hd)), offsets([n, n]), [held, held // 3], n > 1, max_q=n)
 
 
 @pytest.mark.parametrize("form", FORMS)

@@ -97,6 +97,39 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
         assert e.value.code == B.CF_ERR_ARG
 
 
+def plan(form=-1, c=None, **q):
+    out = B.cf_kv_attention_plan()
+    rc = B.lib().cf_plan_kv_attention(C.byref(c or cache()), C.byref(query(**q)), form, C.byref(out))
+    return rc, out
+
+
+def test_plans_are_host_arithmetic_and_say_what_workspace_a_form_needs():
+    ws = C.c_uint64()
+    for form in (-1, 0, 1, 2, 3):
+        rc, p = plan(form)
+        assert rc == B.CF_OK and (form < 0 or p.form == form) and p.columns == (256 if p.form >= 2 else 32) and p.workgroups > 0
+        assert (p.workspace_bytes == 0) == (p.form in (1, 3))
+        if form < 0:
+            assert B.lib().cf_kv_attention_workspace(C.byref(cache()), C.byref(query()), C.byref(ws)) == B.CF_OK and ws.value == p.workspace_bytes
+        # an operand short or misaligned is refused, and so is a form that is none
+        if p.workspace_bytes:
+            for at, size in ((None, p.workspace_bytes), (HERE * 16 + 128, p.workspace_bytes), (HERE * 16, p.workspace_bytes - 1)):
+                assert B.lib().cf_op_kv_attention_form(C.byref(cache()), C.byref(query()), p.form, at, size, None) == B.CF_ERR_ARG
+    assert plan(4)[0] == B.CF_ERR_ARG and plan(-2)[0] == B.CF_ERR_ARG
+    assert B.lib().cf_op_kv_attention_form(C.byref(cache()), C.byref(query()), -1, HERE * 16, 1 << 40, None) == B.CF_ERR_ARG
+    # a call without a workspace that needs one
+    big = cache(table_width=4096)
+    assert B.lib().cf_kv_attention_workspace(C.byref(big), C.byref(query(n_tokens=3)), C.byref(ws)) == B.CF_OK and ws.value > 0
+    assert B.lib().cf_kv_attention(C.byref(big), C.byref(query(n_tokens=3)), None, 0, None) == B.CF_ERR_ARG
+
+
+def test_the_most_queries_of_a_sequence_count_for_the_plan():
+    """Single tokens of many sequences are few columns each; as many queries of one sequence, over as many tokens, are many."""
+    wide = cache(n_seqs=64, table_width=512, heads=8)
+    assert plan(c=wide, n_tokens=64, heads=8, max_q=1)[1].columns == 32
+    assert plan(c=cache(n_seqs=1, table_width=512, heads=8), n_tokens=2000, heads=8)[1].columns == 256
+
+
 def test_the_helpers_know_the_format():
     """The tests' own e4m3 table and power rule, against torch's type and by hand."""
     every = torch.arange(256, dtype=torch.uint8)
