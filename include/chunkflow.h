@@ -374,8 +374,8 @@ typedef struct {
 int cf_kv_append(const cf_kv_cache* cache, const cf_kv_new* tokens, void* stream);
 /* o = softmax(scale * q K^T) V for rows [cu[b], cu[b+1]) of q over the tokens [0, lens[b]) of sequence b (lens AFTER an append), query head i
  * reading the cache's head i / (heads / cache heads).  causal: query j of n sees the tokens up to lens[b] - n + j.  A query that
- * sees none gets zeros.  Rows of o outside [cu[0], cu[n_seqs]) stay as they are.  Tokens that a query does not see take no part,
- * whatever their codes.  Accumulated in fp32; weights are rounded to bf16 for the second product.
+ * sees none gets zeros (and one all of whose scores are -inf).  Rows of o outside [cu[0], cu[n_seqs]) stay as they are; o must not overlap q.
+ * Tokens that a query does not see take no part, whatever their codes.  Accumulated in fp32; weights are rounded to bf16 for the second product.
  * workspace: at least cf_kv_attention_workspace bytes, 256-byte aligned, nothing to initialise; calls that may overlap need one each.
  * max_q: the most queries any sequence has; only plans the launch (0: n_tokens), and results do not depend on it being right beyond
  * rounding.  With the same sizes and strides a call can be captured and replayed on changed tables, lengths and offsets. */

@@ -8,6 +8,7 @@
 #include "../../include/chunkflow_diag.h"
 #include "context.h"
 #include "kv_tile.h"
+#include "rows.h"
 
 namespace {
 
@@ -886,6 +887,10 @@ static int attend(const char* name, const cf_kv_cache* cache, const cf_kv_query*
         return cf_fail(nullptr, CF_ERR_ARG, "%s: q and o must be 16-byte aligned, offsets and lengths 4", name);
     for (const int64_t st : {x->q_row, x->q_head, x->o_row, x->o_head})
         if (st < 0 || st > (int64_t)1 << 40 || st % 8) return cf_fail(nullptr, CF_ERR_ARG, "%s: strides must be multiples of 16 bytes and not negative", name);
+    // pieces of one column tile may read its queries at any time
+    const Rows q = {x->q, x->n_tokens, x->q_row, x->heads, x->q_head, cache->head_dim, 2}, o = {x->o, x->n_tokens, x->o_row, x->heads, x->o_head, cache->head_dim, 2};
+    if (!o.apart()) return cf_fail(nullptr, CF_ERR_ARG, "%s: outputs overlap one another", name);
+    if (rows_meet(q, o)) return cf_fail(nullptr, CF_ERR_ARG, "%s: o overlaps q", name);
     AttendPlan p;
     if (const char* bad = attend_plan(cache, x, form, &p)) return cf_fail(nullptr, CF_ERR_ARG, "%s: %s", name, bad);
     if (p.bytes && (!workspace || (uintptr_t)workspace % 256 || workspace_bytes < p.bytes))

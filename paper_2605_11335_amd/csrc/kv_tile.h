@@ -165,9 +165,10 @@ struct KvShares {
     int64_t total;
     int wgs;
     __device__ __forceinline__ KvShares(int64_t all, int most, int least) : total(all), wgs((int)max((int64_t)1, min((int64_t)most, (all + least - 1) / least))) {}
-    __device__ __forceinline__ int64_t begin(int w) const { return total * w / wgs; }
+    // total * w / wgs, without the product, which might not fit
+    __device__ __forceinline__ int64_t begin(int w) const { return total / wgs * w + total % wgs * w / wgs; }
     __device__ __forceinline__ int of(int64_t f) const {           // the workgroup with work f
-        int w = (int)(f * wgs / total);
+        int w = min((int)((double)f * wgs / (double)total), wgs - 1);
         while (begin(w + 1) <= f) ++w;
         while (begin(w) > f) --w;
         return w;
@@ -301,11 +302,5 @@ __device__ __forceinline__ void kv_spread_nan(KvState<HD>& st, int d, const floa
     for (int v = 0; v < 16; ++v) st.o[d][v] = hits[v] > 0.0f ? __uint_as_float(0x7fc00000u) : st.o[d][v];
 }
 
-// Two partial results of a column, each against its own reference, brought to the higher one.
-struct KvJoin {
-    float m, before, part;
-    __device__ __forceinline__ KvJoin(float m0, float m1) : m(fmaxf(m0, m1)), before(__builtin_amdgcn_exp2f(m0 - m)), part(__builtin_amdgcn_exp2f(m1 - m)) {}
-    __device__ __forceinline__ float operator()(float x0, float x1) const { return fmaf(x1, part, x0 * before); }
-};
 // What divides: 0 where a column has seen nothing.
 __device__ __forceinline__ float kv_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }

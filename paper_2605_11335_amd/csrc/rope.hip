@@ -3,6 +3,7 @@
 
 #include "context.h"
 #include "rope.h"
+#include "rows.h"
 
 namespace {
 
@@ -114,14 +115,6 @@ void launch(const RopeArgs& a, bool far, dim3 grid, hipStream_t s) {
     }
 }
 
-// bytes [lo, hi) that an operand's rows and heads cover
-struct Span { const char *lo, *hi; };
-Span span(const void* p, int64_t n, int64_t row, int64_t heads, int64_t head, int hd, int es) {
-    const char* lo = (const char*)p;
-    return {lo, lo + ((n - 1) * row + (heads - 1) * head + hd) * es};
-}
-bool meet(const Span& a, const Span& b) { return a.lo < b.hi && b.lo < a.hi; }
-
 }  // namespace
 
 extern "C" int cf_rope_plan(int32_t head_dim, int32_t n_axes, const int32_t* axis_pairs, const double* theta, cf_rope* out) {
@@ -153,8 +146,8 @@ extern "C" int cf_rope_tables(const cf_rope* rope, const int32_t* pos, int64_t n
     if (!pos || !cos_out || !sin_out) return cf_fail(nullptr, CF_ERR_ARG, "rope_tables: null operand");
     if (((uintptr_t)cos_out | (uintptr_t)sin_out) % 16 || (uintptr_t)pos % 4) return cf_fail(nullptr, CF_ERR_ARG, "rope_tables: tables must be 16-byte aligned, positions 4");
     const int64_t bytes = n * (rope->head_dim / 2) * 4, pos_bytes = n * rope->n_axes * 4;
-    const Span c = {(char*)cos_out, (char*)cos_out + bytes}, s = {(char*)sin_out, (char*)sin_out + bytes}, p = {(const char*)pos, (const char*)pos + pos_bytes};
-    if (meet(c, s) || meet(c, p) || meet(s, p)) return cf_fail(nullptr, CF_ERR_ARG, "rope_tables: operands overlap");
+    auto meet = [](const void* p, int64_t n, const void* q, int64_t m) { return (const char*)p < (const char*)q + m && (const char*)q < (const char*)p + n; };
+    if (meet(cos_out, bytes, sin_out, bytes) || meet(cos_out, bytes, pos, pos_bytes) || meet(sin_out, bytes, pos, pos_bytes)) return cf_fail(nullptr, CF_ERR_ARG, "rope_tables: operands overlap");
     const int rows = 2048 / rope->head_dim;
     const dim3 grid((unsigned)((n + rows - 1) / rows));
     if (rope->head_dim == 128) hipLaunchKernelGGL(rope_tables_kernel<128>, grid, dim3(256), 0, (hipStream_t)stream, *rope, pos, n, cos_out, sin_out);
@@ -173,7 +166,7 @@ extern "C" int cf_rope_apply(const cf_rope* rope, const int32_t* pos, int64_t n,
     if (!pos || (uintptr_t)pos % 4) return cf_fail(nullptr, CF_ERR_ARG, "rope_apply: null or misaligned positions");
     const int es = dtype == CF_BF16 ? 2 : 4, hd = rope->head_dim;
     RopeArgs a = {};
-    Span in[2], out[2];
+    Rows in[2], out[2];
     for (int i = 0; i < n_ops; ++i) {
         const cf_rope_operand& o = ops[i];
         if (!o.x || !o.y) return cf_fail(nullptr, CF_ERR_ARG, "rope_apply: null operand");
@@ -181,30 +174,17 @@ extern "C" int cf_rope_apply(const cf_rope* rope, const int32_t* pos, int64_t n,
         for (const int64_t st : {o.x_row, o.x_head, o.y_row, o.y_head})
             if (st < 0 || st > (int64_t)1 << 40 || st * es % 16) return cf_fail(nullptr, CF_ERR_ARG, "rope_apply: strides must be multiples of 16 bytes and not negative");
         if (((uintptr_t)o.x | (uintptr_t)o.y) % 16) return cf_fail(nullptr, CF_ERR_ARG, "rope_apply: operands must be 16-byte aligned");
-        // every output has a place of its own: heads inside a row or rows inside a head
-        const bool rows_outside = o.y_head >= hd && (n == 1 || o.y_row >= (o.heads - 1) * o.y_head + hd);
-        const bool heads_outside = o.y_row >= hd && (o.heads == 1 || o.y_head >= (n - 1) * o.y_row + hd);
-        if (!(rows_outside || heads_outside || (o.heads == 1 && (n == 1 || o.y_row >= hd)))) return cf_fail(nullptr, CF_ERR_ARG, "rope_apply: outputs overlap one another");
-        in[i] = span(o.x, n, o.x_row, o.heads, o.x_head, hd, es);
-        out[i] = span(o.y, n, o.y_row, o.heads, o.y_head, hd, es);
+        in[i] = {o.x, n, o.x_row, o.heads, o.x_head, hd, es};
+        out[i] = {o.y, n, o.y_row, o.heads, o.y_head, hd, es};
+        if (!out[i].apart()) return cf_fail(nullptr, CF_ERR_ARG, "rope_apply: outputs overlap one another");
         const bool in_place = o.x == o.y && o.x_row == o.y_row && o.x_head == o.y_head;
-        if (!in_place && meet(in[i], out[i])) return cf_fail(nullptr, CF_ERR_ARG, "rope_apply: an output overlaps its input; in place means the same pointer and strides");
+        if (!in_place && rows_meet(in[i], out[i])) return cf_fail(nullptr, CF_ERR_ARG, "rope_apply: an output overlaps its input; in place means the same pointer and strides");
         a.op[i] = o;
         a.heads += o.heads;
     }
-    // q and k may be columns of one row, so only spans of like strides can be told apart by their places: else they must not meet
     if (n_ops == 2)
         for (int i = 0; i < 2; ++i)
-            for (const Span* s : {&in[1 - i], &out[1 - i]}) {
-                const cf_rope_operand &o = ops[i], &p = ops[1 - i];
-                if (!meet(out[i], *s)) continue;
-                const bool of_out = s == &out[1 - i];
-                const int64_t row = of_out ? p.y_row : p.x_row, head = of_out ? p.y_head : p.x_head;
-                const int64_t apart = ((const char*)(of_out ? p.y : p.x) - (const char*)o.y) / es;      // columns of one row, in elements
-                const int64_t width_o = (o.heads - 1) * o.y_head + hd, width_p = (p.heads - 1) * head + hd;
-                const bool beside = row == o.y_row && (apart >= 0 ? apart >= width_o && apart + width_p <= row : -apart >= width_p && -apart + width_o <= row);
-                if (!beside) return cf_fail(nullptr, CF_ERR_ARG, "rope_apply: an output overlaps the other operand");
-            }
+            if (rows_meet(out[i], in[1 - i]) || rows_meet(out[i], out[1 - i])) return cf_fail(nullptr, CF_ERR_ARG, "rope_apply: an output overlaps the other operand");
     a.r = *rope;
     a.pos = pos;
     a.n = n;

@@ -68,6 +68,16 @@ def test_queries_that_are_refused(bad):
     assert b"kv_attention" in B.lib().cf_last_error(None)
 
 
+@pytest.mark.parametrize("o", [dict(o=HERE * 5), dict(o=HERE * 5 + 1024), dict(o_row=512), dict(o_head=64), dict(q_row=2048, o_row=2048, o=HERE * 5 + 1024)])
+def test_outputs_over_queries_or_over_one_another(o):
+    """In place, half over the queries, rows and heads over one another, and columns of one row that meet by a head; columns side by side are in order."""
+    beside = query(q_row=2048, o_row=2048, o=HERE * 5 + 2048)
+    assert B.lib().cf_kv_attention(C.byref(cache(table_width=4096)), C.byref(beside), None, 0, None) == B.CF_ERR_ARG
+    assert b"workspace" in B.lib().cf_last_error(None)             # (what comes after these checks)
+    assert B.lib().cf_kv_attention(C.byref(cache(table_width=4096)), C.byref(query(**o)), None, 0, None) == B.CF_ERR_ARG
+    assert b"overlap" in B.lib().cf_last_error(None)
+
+
 def test_nothing_to_do_is_no_error():
     assert B.lib().cf_kv_append(C.byref(cache()), C.byref(new(n_tokens=0)), None) == B.CF_OK
     assert B.lib().cf_kv_append(C.byref(cache(n_seqs=0)), C.byref(new()), None) == B.CF_OK
