@@ -720,8 +720,9 @@ __global__ __launch_bounds__(LANES) void kv_join_kernel(AttendArgs a) {
             __syncthreads();
         }
     }
-    int G = 1;
-    while (2 * G * cols * QUADS <= LANES && G < pieces) G *= 2;
+    int G = 1;                                                 // (two pieces of many columns: as kv_attend_many_kernel joins them, one after the other)
+    if (COLS == 32 || pieces > 2)
+        while (2 * G * cols * QUADS <= LANES && G < pieces) G *= 2;
     if (G == 1) {
         floatx4 v[TIMES];
         float sum[TIMES];

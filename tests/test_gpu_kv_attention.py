@@ -1,4 +1,6 @@
 """Attention over a paged 8-bit cache against the definition in 64 bits: ragged, empty, causal, holes in the table, codes that nobody may see."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -276,6 +278,29 @@ def test_the_same_call_gives_the_same_bits(n, heads, form):
     side = torch.cuda.Stream()
     for stream in (None, side, None, None):
         assert np.array_equal(first, run(cache, bits, offsets([n] * 2), [5000, 4321], dev=dev, max_q=n, stream=stream, form=form))
+
+
+@pytest.mark.parametrize("hd,heads", [(64, 1), (64, 8), (128, 1), (128, 4), (128, 5)])
+def test_a_column_tile_in_two_pieces_has_one_result(hd, heads):
+    """128 sequences of the same tokens, each the work of two of 256 shares, which either the first share's workgroup or the joining kernel puts together:
+    no matter which.  Values and scores are such that the halves all but cancel and the last bit of a product is seen."""
+    rng = np.random.default_rng(heads)
+    seqs, held = 128, 640
+    cache = Cache(rng, seqs, 1, hd, 64, held)
+    late = np.zeros((cache.pages, 1, 1, 1, 1), bool)
+    late[cache.table[:, held // 128:].ravel()] = True
+    cache.k[:] = 0
+    cache.k[..., 0, :, 0] = np.where(late[..., 0], 0, 0x38)              # 1 or 0 in the first dim: scores q and 0
+    cache.v[:] = np.where(late, 0xb8, 0x30)                              # -1, 1 / 2
+    cache.scales[:] = 127
+    q = bf16_round(np.ones((seqs, heads, hd)))[1]
+    dev = cache.device(B)
+    shape = dev_bits(q).view(torch.bfloat16)
+    assert B.cf_plan_kv_attention(dev, shape, 1, 2).workgroups == 2 * seqs
+    for ppm in (5, 10, 20, 40):
+        for _ in range(4):
+            got = run(cache, q, offsets([1] * seqs), [held] * seqs, scale=math.log(2) * (1 + ppm * 1e-6), dev=dev, max_q=1, form=2)
+            assert (got == got[0, 0, 0]).all(), np.unique(got)
 
 
 def test_the_planner_takes_every_form():
