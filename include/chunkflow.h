@@ -325,7 +325,8 @@ int cf_rope_plan(int32_t head_dim, int32_t n_axes, const int32_t* axis_pairs, co
 int cf_rope_tables(const cf_rope* rope, const int32_t* pos, int64_t n, float* cos_out, float* sin_out, void* stream);
 /* y = x turned, for one or two operands (q and k) of type `dtype` in one launch: [n, heads, head_dim], the last dimension dense, the
  * others at any strides (elements, not negative, multiples of 16 bytes; pointers 16-byte aligned).  inverse: turned back, which is also the
- * gradient of x from that of y.  In place: y = x with the same strides; outputs may otherwise overlap nothing.  Computed in fp32, rounded once. */
+ * gradient of x from that of y.  In place: y = x with the same strides; outputs may otherwise overlap nothing.  Computed in fp32, rounded once.
+ * n: less than 2^24 (tables: 2^28 - 16). */
 typedef struct {
     const void* x;
     void* y;
@@ -359,7 +360,8 @@ typedef struct {
  * given.  lens is what the sequences hold BEFORE the call and is not changed.  Rows outside [cu[0], cu[n_seqs]) are not read, tokens that
  * the table has no room for are dropped.  The power of two of a group is the least that holds the largest value ( |a| + |b| of a pair that is
  * turned) of its new tokens, and no less than that of the tokens it held; those are then requantised.  What is not finite is stored as NaN and takes
- * no part in that.  A page that tokens are appended to belongs to one sequence only (full pages may be shared).  cu must not decrease. */
+ * no part in that.  A page that tokens are appended to belongs to one sequence only (full pages may be shared).  cu must not decrease.
+ * n_tokens / 16 + 2 n_seqs: less than 2^24. */
 typedef struct {
     const void* k;               /* [n_tokens, heads, head_dim] of `dtype`, the last dimension dense; strides in elements,   */
     const void* v;               /*   not negative, multiples of 16 bytes; pointers 16-byte aligned                          */
@@ -375,7 +377,8 @@ int cf_kv_append(const cf_kv_cache* cache, const cf_kv_new* tokens, void* stream
 /* o = softmax(scale * q K^T) V for rows [cu[b], cu[b+1]) of q over the tokens [0, lens[b]) of sequence b (lens AFTER an append), query head i
  * reading the cache's head i / (heads / cache heads).  causal: query j of n sees the tokens up to lens[b] - n + j.  A query that
  * sees none gets zeros (and one all of whose scores are -inf).  Rows of o outside [cu[0], cu[n_seqs]) stay as they are; o must not overlap q.
- * Tokens that a query does not see take no part, whatever their codes.  Accumulated in fp32; weights are rounded to bf16 for the second product.
+ * Tokens that a query does not see take no part, whatever their codes.  Accumulated in fp32, by weights of up to 2^20 that the end divides by their sum (values past 2^100 may become infinite); weights are rounded to bf16
+ * for the second product.
  * workspace: at least cf_kv_attention_workspace bytes, 256-byte aligned, nothing to initialise; calls that may overlap need one each.
  * max_q: the most queries any sequence has; only plans the launch (0: n_tokens), and results do not depend on it being right beyond
  * rounding.  With the same sizes and strides a call can be captured and replayed on changed tables, lengths and offsets. */

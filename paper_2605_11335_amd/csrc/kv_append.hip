@@ -11,6 +11,7 @@
 #include "context.h"
 #include "kv_cache.h"
 #include "rope.h"
+#include "rows.h"
 
 namespace {
 
@@ -247,7 +248,7 @@ extern "C" int cf_kv_append(const cf_kv_cache* cache, const cf_kv_new* x, void* 
         if (!x->pos) return cf_fail(nullptr, CF_ERR_ARG, "kv_append: a rotation without positions");
     }
     const int64_t items = x->n_tokens / 16 + 2ll * cache->n_seqs;
-    if (items > 0x7fffffff) return cf_fail(nullptr, CF_ERR_ARG, "kv_append: too many tokens and sequences");
+    if (items > MOST_WGS) return cf_fail(nullptr, CF_ERR_ARG, "kv_append: too many tokens and sequences");
     AppendArgs a = {};
     a.c = kv_view(*cache);
     if (x->rope) a.r = *x->rope;

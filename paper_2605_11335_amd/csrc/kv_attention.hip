@@ -844,7 +844,7 @@ const char* attend_plan(const cf_kv_cache* c, const cf_kv_query* x, int form, At
     // One column tile per sequence and key head reads every code once.  32 ragged sequences of up to 8201 tokens x 8 heads 63.7 us, through the caches 72.9; one of
     // 131001 x 12 73.6 / 83.0.  (64 MiB: twice what the L2 caches hold.)
     p->far = !p->many && most <= 32 && seqs * tiles * c->heads > (64ll << 20) / (2 * KV_TILE * c->head_dim);
-    p->wgs = p->whole ? (int)from_all(p->cols) : p->many ? MANY_WGS : FEW_WGS;         // (a workgroup without work ends at once)
+    p->wgs = p->whole ? (int)std::min<int64_t>(from_all(p->cols), 1 << 20) : p->many ? MANY_WGS : FEW_WGS;         // (one without work ends at once; past 2^20 one has several)
     const uint64_t slots = p->whole ? 0 : 2ull * p->wgs * p->cols;
     p->ml_offset = slots * c->head_dim * 4;
     p->cuts_offset = p->ml_offset + slots * 2 * 4;

@@ -141,14 +141,14 @@ extern "C" int cf_rope_plan(int32_t head_dim, int32_t n_axes, const int32_t* axi
 
 extern "C" int cf_rope_tables(const cf_rope* rope, const int32_t* pos, int64_t n, float* cos_out, float* sin_out, void* stream) {
     if (const char* bad = rope_bad(rope)) return cf_fail(nullptr, CF_ERR_ARG, "rope_tables: %s", bad);
-    if (n < 0 || n > 0x7fffffff) return cf_fail(nullptr, CF_ERR_ARG, "rope_tables: %lld rows", (long long)n);
+    const int rows = 2048 / rope->head_dim;
+    if (n < 0 || n > MOST_WGS * rows) return cf_fail(nullptr, CF_ERR_ARG, "rope_tables: %lld rows", (long long)n);
     if (n == 0) return CF_OK;
     if (!pos || !cos_out || !sin_out) return cf_fail(nullptr, CF_ERR_ARG, "rope_tables: null operand");
     if (((uintptr_t)cos_out | (uintptr_t)sin_out) % 16 || (uintptr_t)pos % 4) return cf_fail(nullptr, CF_ERR_ARG, "rope_tables: tables must be 16-byte aligned, positions 4");
     const int64_t bytes = n * (rope->head_dim / 2) * 4, pos_bytes = n * rope->n_axes * 4;
     auto meet = [](const void* p, int64_t n, const void* q, int64_t m) { return (const char*)p < (const char*)q + m && (const char*)q < (const char*)p + n; };
     if (meet(cos_out, bytes, sin_out, bytes) || meet(cos_out, bytes, pos, pos_bytes) || meet(sin_out, bytes, pos, pos_bytes)) return cf_fail(nullptr, CF_ERR_ARG, "rope_tables: operands overlap");
-    const int rows = 2048 / rope->head_dim;
     const dim3 grid((unsigned)((n + rows - 1) / rows));
     if (rope->head_dim == 128) hipLaunchKernelGGL(rope_tables_kernel<128>, grid, dim3(256), 0, (hipStream_t)stream, *rope, pos, n, cos_out, sin_out);
     else hipLaunchKernelGGL(rope_tables_kernel<64>, grid, dim3(256), 0, (hipStream_t)stream, *rope, pos, n, cos_out, sin_out);
@@ -161,7 +161,7 @@ extern "C" int cf_rope_apply(const cf_rope* rope, const int32_t* pos, int64_t n,
     if (const char* bad = rope_bad(rope)) return cf_fail(nullptr, CF_ERR_ARG, "rope_apply: %s", bad);
     if (dtype != CF_BF16 && dtype != CF_F32) return cf_fail(nullptr, CF_ERR_ARG, "rope_apply: type %d is neither CF_BF16 nor CF_F32", dtype);
     if (!ops || n_ops < 1 || n_ops > 2) return cf_fail(nullptr, CF_ERR_ARG, "rope_apply: one or two operands");
-    if (n < 0 || n > 0x7fffffff) return cf_fail(nullptr, CF_ERR_ARG, "rope_apply: %lld rows", (long long)n);
+    if (n < 0 || n > MOST_WGS) return cf_fail(nullptr, CF_ERR_ARG, "rope_apply: %lld rows", (long long)n);
     if (n == 0) return CF_OK;
     if (!pos || (uintptr_t)pos % 4) return cf_fail(nullptr, CF_ERR_ARG, "rope_apply: null or misaligned positions");
     const int es = dtype == CF_BF16 ? 2 : 4, hd = rope->head_dim;

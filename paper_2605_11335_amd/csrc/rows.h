@@ -1,6 +1,8 @@
-// Where the rows of an operand [n, heads, width] lie, for the checks of entry points that write one while others are read.
+// Host checks of operands: where the rows of one [n, heads, width] lie, for entry points that write one while others are read, and what fits a launch.
 #pragma once
 #include <stdint.h>
+
+constexpr int64_t MOST_WGS = (1 << 24) - 1;          // of 256 lanes in one launch
 
 struct Rows {
     const void* p;

@@ -280,6 +280,20 @@ def test_the_same_call_gives_the_same_bits(n, heads, form):
         assert np.array_equal(first, run(cache, bits, offsets([n] * 2), [5000, 4321], dev=dev, max_q=n, stream=stream, form=form))
 
 
+@pytest.mark.parametrize("form", [0, 1, 2, 3])
+def test_outputs_past_4_gib(form):
+    """2^25 columns: in the form of a workgroup for each column tile of 32, several to a workgroup.  One token: every query's output is its value."""
+    rng = np.random.default_rng(form)
+    cache = Cache(rng, 1, 1, 64, 16, 16, fill="small")
+    n = 2 ** 20 + 5
+    q = torch.ones(n, 32, 64, dtype=torch.bfloat16, device=DEV)
+    o, dev = torch.full_like(q, 7.0), cache.device(B)
+    ws = torch.empty(B.cf_plan_kv_attention(dev, q, n, form).workspace_bytes, dtype=torch.uint8, device=DEV)
+    B.cf_op_kv_attention_form(dev, q, o, lens_t([0, n - 1]), lens_t([1]), form, False, None, n, ws)
+    want = torch.from_numpy(cache.held(0, 1)[1][0, 0]).to(DEV, torch.bfloat16)
+    assert bool((o[:-1] == want).all()) and bool((o[-1] == 7).all())
+
+
 @pytest.mark.parametrize("hd,heads", [(64, 1), (64, 8), (128, 1), (128, 4), (128, 5)])
 def test_a_column_tile_in_two_pieces_has_one_result(hd, heads):
     """128 sequences of the same tokens, each the work of two of 256 shares, which either the first share's workgroup or the joining kernel puts together:

@@ -51,6 +51,12 @@ def test_appends_that_are_refused(bad):
     assert b"kv_append" in B.lib().cf_last_error(None)
 
 
+@pytest.mark.parametrize("n_tokens,n_seqs", [(2 ** 28, 1), (2 ** 31 - 1, 1), (9, 2 ** 23), (2 ** 27, 2 ** 22)])
+def test_more_tokens_than_a_launch_has_room_for(n_tokens, n_seqs):
+    assert B.lib().cf_kv_append(C.byref(cache(n_seqs=n_seqs)), C.byref(new(n_tokens=n_tokens)), None) == B.CF_ERR_ARG
+    assert b"too many" in B.lib().cf_last_error(None)
+
+
 def test_rotations_that_do_not_fit_the_cache():
     right, wrong = B.cf_rope_plan(128, [64]), B.cf_rope_plan(64, [32])
     for rope, pos in ((wrong, HERE * 9), (right, None), (right, HERE * 9 + 2), (B.cf_rope(), HERE * 9)):
@@ -138,6 +144,11 @@ def test_the_most_queries_of_a_sequence_count_for_the_plan():
     wide = cache(n_seqs=64, table_width=512, heads=8)
     assert plan(c=wide, n_tokens=64, heads=8, max_q=1)[1].columns == 32
     assert plan(c=cache(n_seqs=1, table_width=512, heads=8), n_tokens=2000, heads=8)[1].columns == 256
+
+
+def test_launches_have_room_for_any_number_of_queries():
+    for form in range(4):
+        assert 0 < plan(form, n_tokens=2 ** 27, heads=8)[1].workgroups <= 2 ** 20
 
 
 def test_the_helpers_know_the_format():

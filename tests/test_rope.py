@@ -73,6 +73,14 @@ def test_tables_that_are_refused(args):
     assert b"rope_tables" in B.lib().cf_last_error(None)
 
 
+@pytest.mark.parametrize("hd,n", [(64, 2 ** 24 * 32), (128, 2 ** 24 * 16), (128, 2 ** 31 - 1), (128, 2 ** 40)])
+def test_more_rows_than_a_launch_has_room_for(hd, n):
+    rope = B.cf_rope_plan(hd, [32])
+    assert B.lib().cf_rope_tables(C.byref(rope), HERE, n, HERE << 30, HERE << 31, None) == B.CF_ERR_ARG and b" rows" in B.lib().cf_last_error(None)
+    for rows in (n, 2 ** 24):
+        assert apply_code(operand(), rope=rope, n=rows) == B.CF_ERR_ARG and b" rows" in B.lib().cf_last_error(None)
+
+
 def test_the_binding_refuses_tensors_that_do_not_fit():
     rope = B.cf_rope_plan(64, [16, 16])
     pos, q = torch.zeros(6, 2, dtype=torch.int32), torch.zeros(6, 3, 64)
