@@ -233,8 +233,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attend_few_kernel(Attend
     while (f < f1) {
         q = kv_find<32>(a, f);
         const int64_t q_end = q.first + q.head() * a.c.heads;
-        while (f < f1 && f < q_end) {
-            p = kv_piece<32>(a, q, f, f1);
+        const int64_t to = min(f1, q_end);
+        for (KvPiece n = kv_piece<32>(a, q, f, f1); f < to;) {
+            p = n;
+            if (p.next < to) n = kv_next<32>(a, q, p, f1);
             const int h = p.h, c = p.c;
             const KvColumn col = kv_column(a, q, h, 32 * c + lj);
             for (int k = wave; k < HD / 16; k += FEW_WAVES)
@@ -315,6 +317,31 @@ __device__ __forceinline__ int anew(int x) {
 template <int HD>
 __device__ __forceinline__ int many_row(int col, int c) { return col * (2 * HD) + ((c ^ (col & (HD / 8 - 1))) << 4); }
 
+// The columns whose rows a lane has a chunk of, of a wave's 32: every (512 / HD)-th, from the lane's first one on.  Where a column's query or output lies takes a
+// division and products of 64 bits; from one to the next it is one of two steps.
+template <int HD, class T>
+struct ManyRow {
+    int r, head, last, times, step_heads;
+    T* row;                                            // of column r, or of one before it if there is no column r
+    int64_t step, wrap;
+    __device__ __forceinline__ ManyRow(const AttendArgs& a, const KvSeq& q, int h, int col0, int ln, T* base, int64_t row_stride, int64_t head_stride)
+        : r(ln / (HD / 8)), last(q.n * a.times - col0 - 1), times(a.times), step_heads(a.step_heads) {
+        const KvColumn c = kv_column(a, q, h, col0 + r);
+        head = c.head - h * a.times;
+        row = base + (int64_t)c.row * row_stride + (int64_t)c.head * head_stride;
+        step = a.step_rows * row_stride + a.step_heads * head_stride;
+        wrap = step + row_stride - a.times * head_stride;
+    }
+    __device__ __forceinline__ void next() {
+        r += 512 / HD;
+        head += step_heads;
+        const bool over = head >= times;
+        head -= over ? times : 0;
+        const int64_t by = over ? wrap : step;
+        row += r <= last ? by : 0;
+    }
+};
+
 // What is on its way for the workgroup's next piece while it finishes one.
 template <int HD, int NW>
 struct ManyAhead {
@@ -370,12 +397,11 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
     // this wave's query rows from memory into LDS, past the registers: a lane fetches the chunk whose place it fills
     auto ask_queries = [&](const KvPiece& p) __attribute__((always_inline)) {
         const int ln = anew(lane), col0 = 32 * NW * p.c + 32 * wave;
+        ManyRow<HD, const bf16> at(a, q, p.h, col0, ln, a.q, a.q_row, a.q_head);
 #pragma unroll
-        for (int i = 0; i < HD / 16; ++i) {
-            const int r = i * (512 / HD) + ln / (HD / 8), ch = ln % (HD / 8) ^ (r & (HD / 8 - 1));
-            const KvColumn c = kv_column(a, q, p.h, col0 + r);
-            const bf16* const from = a.q + (int64_t)c.row * a.q_row + (int64_t)c.head * a.q_head + ch * 8;
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+        for (int i = 0; i < HD / 16; ++i, at.next()) {
+            const int ch = ln % (HD / 8) ^ (at.r & (HD / 8 - 1));
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(at.row + ch * 8),
                                              (__attribute__((address_space(3))) void*)(sh.rows[wave] + i * 1024), 16, 0, 0);
         }
     };
@@ -598,7 +624,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
         for (bool ready = false; f < q_end;) {
             p = n;
             bool more = p.next < q_end;
-            if (more) n = kv_piece<COLS>(a, q, p.next, f1);
+            if (more) n = kv_next<COLS>(a, q, p, f1);
             more = more && n.t0 < n.t1;
             KvState<HD> st;
             if (p.t0 < p.t1) {
@@ -644,12 +670,12 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
                 }
                 lds_order();
                 __builtin_amdgcn_sched_barrier(0);
+                ManyRow<HD, bf16> to(a, q, p.h, col0, ln, a.o, a.o_row, a.o_head);
 #pragma unroll
-                for (int i = 0; i < HD / 16; ++i) {
-                    const int r = i * (512 / HD) + ln / (HD / 8), ch = ln % (HD / 8);
-                    const KvColumn to = kv_column(a, q, p.h, col0 + r);
-                    const bf16x8 x = *(const bf16x8*)(rows + many_row<HD>(r, ch));
-                    if (r < cols) __builtin_nontemporal_store(x, (bf16x8*)(a.o + (int64_t)to.row * a.o_row + (int64_t)to.head * a.o_head + ch * 8));
+                for (int i = 0; i < HD / 16; ++i, to.next()) {
+                    const int ch = ln % (HD / 8);
+                    const bf16x8 x = *(const bf16x8*)(rows + many_row<HD>(to.r, ch));
+                    if (to.r < cols) __builtin_nontemporal_store(x, (bf16x8*)(to.row + ch * 8));
                 }
                 lds_order();
             } else if (cols > 0) {
@@ -902,6 +928,7 @@ static int attend(const char* name, const cf_kv_cache* cache, const cf_kv_query*
     a.q_row = x->q_row; a.q_head = x->q_head; a.o_row = x->o_row; a.o_head = x->o_head;
     a.cu = x->cu; a.lens = x->lens;
     a.n_tokens = x->n_tokens; a.heads = x->heads; a.times = x->heads / cache->heads;
+    a.step_rows = 512 / cache->head_dim / a.times; a.step_heads = 512 / cache->head_dim % a.times;
     a.causal = x->causal != 0;
     a.whole = p.whole;
     a.c2 = x->scale * 1.4426950408889634f;

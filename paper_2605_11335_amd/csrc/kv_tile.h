@@ -22,6 +22,7 @@ struct AttendArgs {
     int64_t q_row, q_head, o_row, o_head;
     const int32_t *cu, *lens;
     int32_t n_tokens, heads, times;        // times: query heads per key head
+    int32_t step_rows, step_heads;         // 512 / head_dim columns further on (many columns: from one row of 16-byte chunks of a lane's to its next)
     int32_t causal;
     int32_t whole;                         // no column tile is cut: each is a share of its own
     float c2;                              // scale * log2(e)
@@ -53,6 +54,10 @@ struct KvSeq {
     __device__ __forceinline__ int64_t head() const { return before(ct); }
 };
 
+// x / y of what is not negative; nearly always both have 32 bits, and the division of 64 takes 5 times as long
+__device__ __forceinline__ int64_t kv_div(int64_t x, int64_t y) {
+    return (uint64_t)(x | y) >> 32 ? x / y : (int64_t)((uint32_t)x / (uint32_t)y);
+}
 // values that all lanes agree on, in scalar registers
 __device__ __forceinline__ int64_t kv_lane64(int64_t x, int lane) {
     return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, lane));
@@ -127,17 +132,35 @@ struct KvPiece {
     bool from_start, whole;
     int64_t next, end;                     // where the work after it begins, and where that of its column tile ends
 };
-// The piece of sequence s that begins at f, in a share that ends at f1.
+// The piece of column tile c of head h that begins x of its work behind its beginning, f in all, in a share that ends at f1.
+template <int COLS>
+__device__ __forceinline__ KvPiece kv_part(const AttendArgs& a, const KvSeq& s, int h, int c, int64_t x, int64_t f, int64_t f1) {
+    KvPiece p;
+    p.h = h;
+    p.c = c;
+    const int64_t w = s.w0 + (int64_t)c * s.dw, to = min(w, x + (f1 - f));
+    const int cols = min(COLS, s.n * a.times - COLS * c);
+    const int last = (int)((uint32_t)(COLS * c + cols - 1) / (uint32_t)a.times);
+    const int end = a.causal ? min(s.len, s.len - s.n + last + 1) : s.len;           // of the keys that any column sees
+    const int tiles = (max(end, 0) + KV_TILE - 1) / KV_TILE;
+    p.t0 = x == 0 ? 0 : (int)kv_div(x * tiles, w);
+    p.t1 = to == w ? tiles : (int)kv_div(to * tiles, w);
+    p.from_start = x == 0;
+    p.whole = x == 0 && to == w;
+    p.next = f + (to - x);
+    p.end = f + (w - x);
+    return p;
+}
+// The piece of sequence s that begins at f,
 template <int COLS>
 __device__ __forceinline__ KvPiece kv_piece(const AttendArgs& a, const KvSeq& s, int64_t f, int64_t f1) {
-    KvPiece p;
     const int64_t per = s.head();
     int64_t x = f - s.first;
-    p.h = (int)(x / per);
-    x -= p.h * per;
+    const int h = (int)kv_div(x, per);
+    x -= h * per;
     int lo = 0, hi = s.ct - 1;             // the last column tile that begins at or before x
     if (s.dw == 0) {
-        lo = (int)(x / s.w0);
+        lo = (int)kv_div(x, s.w0);
     } else {
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
@@ -145,20 +168,13 @@ __device__ __forceinline__ KvPiece kv_piece(const AttendArgs& a, const KvSeq& s,
             else hi = mid - 1;
         }
     }
-    p.c = lo;
-    x -= s.before(p.c);
-    const int64_t w = s.w0 + (int64_t)p.c * s.dw, to = min(w, x + (f1 - f));
-    const int cols = min(COLS, s.n * a.times - COLS * p.c);
-    const int last = (COLS * p.c + cols - 1) / a.times;
-    const int end = a.causal ? min(s.len, s.len - s.n + last + 1) : s.len;           // of the keys that any column sees
-    const int tiles = (max(end, 0) + KV_TILE - 1) / KV_TILE;
-    p.t0 = (int)(x * tiles / w);
-    p.t1 = (int)(to * tiles / w);
-    p.from_start = x == 0;
-    p.whole = x == 0 && to == w;
-    p.next = f + (to - x);
-    p.end = f + (w - x);
-    return p;
+    return kv_part<COLS>(a, s, h, lo, x - s.before(lo), f, f1);
+}
+// and the one after p, the whole of the next column tile or the beginning of it.
+template <int COLS>
+__device__ __forceinline__ KvPiece kv_next(const AttendArgs& a, const KvSeq& s, const KvPiece& p, int64_t f1) {
+    const bool same = p.c + 1 < s.ct;
+    return kv_part<COLS>(a, s, same ? p.h : p.h + 1, same ? p.c + 1 : 0, 0, p.next, f1);
 }
 // Equal shares of all work for up to `most` workgroups, none of less than `least`.
 struct KvShares {
@@ -166,7 +182,10 @@ struct KvShares {
     int wgs;
     __device__ __forceinline__ KvShares(int64_t all, int most, int least) : total(all), wgs((int)max((int64_t)1, min((int64_t)most, (all + least - 1) / least))) {}
     // total * w / wgs, without the product, which might not fit
-    __device__ __forceinline__ int64_t begin(int w) const { return total / wgs * w + total % wgs * w / wgs; }
+    __device__ __forceinline__ int64_t begin(int w) const { 
+        const int64_t each = kv_div(total, wgs);
+        return each * w + kv_div((total - each * wgs) * w, wgs);
+    }
     __device__ __forceinline__ int of(int64_t f) const {           // the workgroup with work f
         int w = min((int)((double)f * wgs / (double)total), wgs - 1);
         while (begin(w + 1) <= f) ++w;
@@ -196,7 +215,7 @@ struct KvColumn {
     bool mine;                             // a column, not padding (which repeats the last one)
 };
 __device__ __forceinline__ KvColumn kv_column(const AttendArgs& a, const KvSeq& s, int h, int col) {
-    const int cols = s.n * a.times, c = min(col, cols - 1), i = c / a.times;
+    const int cols = s.n * a.times, c = min(col, cols - 1), i = (int)((uint32_t)c / (uint32_t)a.times);
     return {s.start + i, h * a.times + (c - i * a.times), a.causal ? min(s.len, s.len - s.n + i + 1) : s.len, col < cols};
 }
 
