@@ -142,7 +142,7 @@ __device__ __forceinline__ void few_sweep(const AttendArgs& a, const KvSeq& q, i
             nth = next();
             if (nth >= 0) load_k(g, p, nth);
             __builtin_amdgcn_sched_barrier(0);
-            kv_softmax<HD>(st, s, a.c2, pf);
+            kv_softmax<HD>(st, s, a.c2, pf, false);
             __builtin_amdgcn_sched_barrier(0);
             values();
             if (nth >= 0) load_v(g, p, nth);
@@ -174,7 +174,7 @@ __device__ __forceinline__ void few_sweep(const AttendArgs& a, const KvSeq& q, i
                 rel[i] = there ? min(max(col.end - from, 0), 16) : 0;
             }
             kv_mask(s, rel);
-            kv_softmax<HD>(st, s, a.c2, pf);
+            kv_softmax<HD>(st, s, a.c2, pf, false);
             __builtin_amdgcn_sched_barrier(0);
             load_v(g, p, nth);
 #pragma unroll
@@ -244,7 +244,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attend_few_kernel(Attend
             __syncthreads();
             KvState<HD> st;
             few_sweep<HD, FAR>(a, q, h, c, p.t0, p.t1, sq, st);
-            const float l = st.l + __shfl_xor(st.l, 32);
+            const float l = kv_sum_halves(st.l);
 #pragma unroll
             for (int i = 0; i < DT * 4; ++i)
                 *(floatx4*)so[wave][i][lane] = floatx4{st.o[i / 4][i % 4 * 4], st.o[i / 4][i % 4 * 4 + 1], st.o[i / 4][i % 4 * 4 + 2], st.o[i / 4][i % 4 * 4 + 3]};
@@ -287,7 +287,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attend_few_kernel(Attend
             f = p.next;
         }
     }
-    if (!a.whole) kv_leave_cut<32>(a, shares, w, q, p, any);
+    if (!a.whole) kv_leave_cut<32>(a, shares, w, q, p);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -408,7 +408,7 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
     auto landed = []() __attribute__((always_inline)) { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
     if (tid < 2) sh.flags[tid].nan = 0;
     // tiles [t0, t_plain) are seen whole by every column of the workgroup and have all their pages
-    const int least = a.causal ? min(q.len, q.len - q.n + 32 * NW * p.c / a.times + 1) : q.len;
+    const int least = kv_end(a, q, (int)((uint32_t)(32 * NW * p.c) / (uint32_t)a.times));
     int t_plain = max(t0, min(t1, max(least, 0) / KV_TILE));
     if (!ready) {
         look_up(t0, page);
@@ -546,7 +546,7 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
         scores(buf);
         first_values(buf);
         __builtin_amdgcn_sched_barrier(0);
-        kv_softmax<HD>(st, s, a.c2, pf);
+        kv_softmax<HD>(st, s, a.c2, pf, t == t0);
         __builtin_amdgcn_sched_barrier(0);
         values(buf);
         __syncthreads();                               // tile t + 1 is in its buffer, that of t is free
@@ -562,7 +562,7 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
             for (int i = 0; i < 2; ++i) rel[i] = min((int)(there >> (8 * (2 * i + lg)) & 255u), min(max(col.end - (t * KV_TILE + 32 * i + 16 * lg), 0), 16));
             kv_mask(s, rel);
             __builtin_amdgcn_sched_barrier(0);
-            kv_softmax<HD>(st, s, a.c2, pf);
+            kv_softmax<HD>(st, s, a.c2, pf, t == t0);
             __builtin_amdgcn_sched_barrier(0);
             if (__builtin_amdgcn_readfirstlane(sh.flags[buf].nan) == (uint32_t)t + 1) {
 #pragma unroll
@@ -635,7 +635,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
                 ready = false;
             }
             const int col0 = COLS * p.c + 32 * wave, cols = min(32, q.n * a.times - col0);
-            float l = st.l + __shfl_xor(st.l, 32);
+            float l = kv_sum_halves(st.l);
             // A column tile of two pieces: the share after this one began with the other, so that it is nearly always there; if so, it is joined here, in the
             // order and with the roundings of kv_join_kernel.
             if (cols > 0 && p.from_start && !p.whole && p.end <= shares.begin(w + 2) &&
@@ -697,7 +697,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
         }
     }
     if (!a.whole) {
-        kv_leave_cut<COLS>(a, shares, w, q, p, any);
+        kv_leave_cut<COLS>(a, shares, w, q, p);
         if (lane == 0) a.joined[w * NW + wave] = joined;
     }
 }
@@ -930,6 +930,7 @@ static int attend(const char* name, const cf_kv_cache* cache, const cf_kv_query*
     a.n_tokens = x->n_tokens; a.heads = x->heads; a.times = x->heads / cache->heads;
     a.step_rows = 512 / cache->head_dim / a.times; a.step_heads = 512 / cache->head_dim % a.times;
     a.causal = x->causal != 0;
+    a.end_least = x->causal ? INT32_MIN : INT32_MAX;
     a.whole = p.whole;
     a.c2 = x->scale * 1.4426950408889634f;
     if (!p.whole) {

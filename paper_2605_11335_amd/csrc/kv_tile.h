@@ -24,6 +24,7 @@ struct AttendArgs {
     int32_t n_tokens, heads, times;        // times: query heads per key head
     int32_t step_rows, step_heads;         // 512 / head_dim columns further on (many columns: from one row of 16-byte chunks of a lane's to its next)
     int32_t causal;
+    int32_t end_least;                     // of the keys that a query sees, before its sequence's length: INT_MAX, causal INT_MIN
     int32_t whole;                         // no column tile is cut: each is a share of its own
     float c2;                              // scale * log2(e)
     float* part_o;                         // results of pieces of a column tile's keys: few columns [column][head_dim], many as they lie in registers,
@@ -126,6 +127,9 @@ __device__ __forceinline__ KvSeq kv_find(const AttendArgs& a, int64_t f) {
     }
 }
 
+// Query row i of sequence s sees keys [0, this).
+__device__ __forceinline__ int kv_end(const AttendArgs& a, const KvSeq& s, int i) { return min(s.len, max(s.len - s.n + i + 1, a.end_least)); }
+
 // A column tile and a share of its keys: tiles [t0, t1) of `tiles`.
 struct KvPiece {
     int h, c, t0, t1;
@@ -141,7 +145,7 @@ __device__ __forceinline__ KvPiece kv_part(const AttendArgs& a, const KvSeq& s, 
     const int64_t w = s.w0 + (int64_t)c * s.dw, to = min(w, x + (f1 - f));
     const int cols = min(COLS, s.n * a.times - COLS * c);
     const int last = (int)((uint32_t)(COLS * c + cols - 1) / (uint32_t)a.times);
-    const int end = a.causal ? min(s.len, s.len - s.n + last + 1) : s.len;           // of the keys that any column sees
+    const int end = kv_end(a, s, last);              // of the keys that any column sees
     const int tiles = (max(end, 0) + KV_TILE - 1) / KV_TILE;
     p.t0 = x == 0 ? 0 : (int)kv_div(x * tiles, w);
     p.t1 = to == w ? tiles : (int)kv_div(to * tiles, w);
@@ -194,11 +198,11 @@ struct KvShares {
     }
 };
 
-// What the last piece of a workgroup's share (and that of a workgroup without one) leaves for the kernel that joins pieces.
+// What the last piece of a workgroup's share (without one: KvPiece{}) leaves for the kernel that joins pieces.
 template <int COLS>
-__device__ __forceinline__ void kv_leave_cut(const AttendArgs& a, const KvShares& shares, int w, const KvSeq& q, const KvPiece& p, bool any) {
+__device__ __forceinline__ void kv_leave_cut(const AttendArgs& a, const KvShares& shares, int w, const KvSeq& q, const KvPiece& p) {
     KvCut cut = {};
-    if (any && p.from_start && !p.whole) {
+    if (p.from_start && !p.whole) {
         const int64_t unit = q.first + p.h * q.head() + q.before(p.c);
         cut.start = q.start;
         cut.n = q.n;
@@ -216,7 +220,7 @@ struct KvColumn {
 };
 __device__ __forceinline__ KvColumn kv_column(const AttendArgs& a, const KvSeq& s, int h, int col) {
     const int cols = s.n * a.times, c = min(col, cols - 1), i = (int)((uint32_t)c / (uint32_t)a.times);
-    return {s.start + i, h * a.times + (c - i * a.times), a.causal ? min(s.len, s.len - s.n + i + 1) : s.len, col < cols};
+    return {s.start + i, h * a.times + (c - i * a.times), kv_end(a, s, i), col < cols};
 }
 
 // ---- a tile
@@ -254,13 +258,23 @@ __device__ __forceinline__ void kv_mask(floatx16 (&s)[2], const int (&rel)[2]) {
         for (int v = 0; v < 16; ++v) s[mt][v] = v < rel[mt] ? s[mt][v] : -INFINITY;
 }
 
+// What the two lanes of a column have, for both of them.
+__device__ __forceinline__ uint32x2 kv_halves(uint32_t x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return uint32x2{r[0], r[1]};
+}
+__device__ __forceinline__ float kv_sum_halves(float x) {
+    const uint32x2 r = kv_halves(__float_as_uint(x));
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 // Weights of a tile: P^T in bf16 as the second contraction takes it, and the sum of the weights as rounded.  The reference is not the
 // running maximum: softmax does not depend on it, and fp32 and bf16 are as exact at 2^19 as at 1.  It stays where it is as long as a lane's 32 weights
 // add up to less than 2^20, which the sum, needed anyway, tells; else it moves to the largest score (always in a column's first tile,
-// where weights against kNoRef are infinite), and what has been summed up is brought to it.
+// where weights against kNoRef are infinite; `fresh`: they need not be computed), and what has been summed up is brought to it.
 template <int HD>
-__device__ __forceinline__ void kv_softmax(KvState<HD>& st, const floatx16 (&s)[2], float c2, bf16x8 (&pf)[4]) {
-    float psum;
+__device__ __forceinline__ void kv_softmax(KvState<HD>& st, const floatx16 (&s)[2], float c2, bf16x8 (&pf)[4], bool fresh) {
+    float psum = 0.0f;
     auto weigh = [&]() __attribute__((always_inline)) {
         float ps[4] = {0.f, 0.f, 0.f, 0.f};
         bf16x2 ones;
@@ -278,15 +292,15 @@ __device__ __forceinline__ void kv_softmax(KvState<HD>& st, const floatx16 (&s)[
             }
         psum = (ps[0] + ps[1]) + (ps[2] + ps[3]);
     };
-    weigh();
-    const bool over = !(psum < 1048576.0f);
+    if (!fresh) weigh();
+    const bool over = fresh || !(psum < 1048576.0f);
     if (__any(over)) {                     // (only the columns that need it move: a column's bits do not depend on those beside it)
         float mx = s[0][0];
 #pragma unroll
         for (int v = 1; v < 32; ++v) mx = fmaxf(mx, s[v >> 4][v & 15]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const int other = __shfl_xor((int)over, 32);
-        const float mc = over || other ? fmaxf(st.mc, mx * c2) : st.mc, f = __builtin_amdgcn_exp2f(st.mc - mc);
+        const uint32x2 both = kv_halves(__float_as_uint(mx)), either = kv_halves(over);
+        mx = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+        const float mc = either[0] | either[1] ? fmaxf(st.mc, mx * c2) : st.mc, f = __builtin_amdgcn_exp2f(st.mc - mc);
         st.mc = mc;
         st.l *= f;
 #pragma unroll
