@@ -224,14 +224,15 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attend_few_kernel(Attend
     __shared__ float sm[FEW_WAVES][32][2];
     __shared__ bf16x8 sq[HD / 16][64];                      // query fragments, the same for all waves
     const int lane = threadIdx.x & 63, lj = lane & 31, lg = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = blockIdx.x;
-    const KvShares shares(kv_total<32>(a), gridDim.x, a.whole ? 1 : FEW_LEAST);
+    const KvScan<32> scan(a, 0);
+    const KvShares shares(kv_total<32>(a, scan), gridDim.x, a.whole ? 1 : FEW_LEAST);
     KvSeq q = {};
     KvPiece p = {};
     const bool any = w < shares.wgs && shares.total > 0;
     int64_t f = any ? shares.begin(w) : 0;
     const int64_t f1 = any ? shares.begin(w + 1) : 0;
+    if (f < f1) q = kv_find<32>(a, f, scan);
     while (f < f1) {
-        q = kv_find<32>(a, f);
         const int64_t q_end = q.first + q.head() * a.c.heads;
         const int64_t to = min(f1, q_end);
         for (KvPiece n = kv_piece<32>(a, q, f, f1); f < to;) {
@@ -286,6 +287,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attend_few_kernel(Attend
             __syncthreads();
             f = p.next;
         }
+        if (f < f1) q = kv_find<32>(a, f, KvScan<32>(a, 0));
     }
     if (!a.whole) kv_leave_cut<32>(a, shares, w, q, p);
 }
@@ -605,7 +607,8 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
     constexpr int DT = HD / 32, COLS = 32 * NW;
     __shared__ ManyShared<HD, NW> sh;
     const int lane = threadIdx.x & 63, lj = lane & 31, lg = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const KvShares shares(kv_total<COLS>(a), gridDim.x, a.whole ? 1 : MANY_LEAST);
+    const KvScan<COLS> scan(a, 0);
+    const KvShares shares(kv_total<COLS>(a, scan), gridDim.x, a.whole ? 1 : MANY_LEAST);
     KvSeq q = {};
     KvPiece p = {};
     const bool any = (int)blockIdx.x < shares.wgs && shares.total > 0;
@@ -613,8 +616,8 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
     int64_t f = any ? shares.begin(w) : 0;
     const int64_t f1 = any ? shares.begin(w + 1) : 0;
     bool joined = false;                               // the last piece, with what follows it
+    if (f < f1) q = kv_find<COLS>(a, f, scan);
     while (f < f1) {
-        q = kv_find<COLS>(a, f);
         const int64_t q_end = min(f1, q.first + q.head() * a.c.heads);
         bool hole = false;
         for (int i = threadIdx.x; i <= (q.len - 1) >> a.c.page_shift; i += 64 * NW) hole |= (uint32_t)a.c.table[(int64_t)q.b * a.c.table_stride + i] >= (uint32_t)a.c.n_pages;
@@ -695,6 +698,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
             }
             f = p.next;
         }
+        if (f < f1) q = kv_find<COLS>(a, f, KvScan<COLS>(a, 0));
     }
     if (!a.whole) {
         kv_leave_cut<COLS>(a, shares, w, q, p);

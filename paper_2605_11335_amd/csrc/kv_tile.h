@@ -109,17 +109,19 @@ struct KvScan {
         return r;
     }
 };
+// All work; `first` is the scan of the first 64 sequences.
 template <int COLS>
-__device__ __forceinline__ int64_t kv_total(const AttendArgs& a) {
-    int64_t t = 0;
-    for (int base = 0; base < a.c.n_seqs; base += 64) t += KvScan<COLS>(a, base).all();
+__device__ __forceinline__ int64_t kv_total(const AttendArgs& a, const KvScan<COLS>& first) {
+    int64_t t = first.all();
+    for (int base = 64; base < a.c.n_seqs; base += 64) t += KvScan<COLS>(a, base).all();
     return t;
 }
-// The sequence with work f, 0 <= f < kv_total.
+// The sequence with work f, 0 <= f < kv_total: of the first 64 as scanned, or behind them.
 template <int COLS>
-__device__ __forceinline__ KvSeq kv_find(const AttendArgs& a, int64_t f) {
-    int64_t before = 0;
-    for (int base = 0;; base += 64) {
+__device__ __forceinline__ KvSeq kv_find(const AttendArgs& a, int64_t f, const KvScan<COLS>& first) {
+    if (const uint64_t m = __ballot(f < first.upto)) return first.pick(a, 0, 0, __builtin_ctzll(m));
+    int64_t before = first.all();
+    for (int base = 64;; base += 64) {
         const KvScan<COLS> s(a, base);
         const uint64_t m = __ballot(f < before + s.upto);
         if (m) return s.pick(a, base, before, __builtin_ctzll(m));
