@@ -358,9 +358,9 @@ struct ManyAhead {
 constexpr int AGENT = 16;                              // cache policy of a buffer access: sc1, past the XCD's L2
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t agent_rsrc(const void* base, int bytes) { return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00020000); }
 
-// Piece p of sequence q.  ready: its query rows are in LDS, its first codes on their way (x).  more: piece n of the same sequence comes next, and is made ready.
+// Piece p of sequence q.  holes: whether a page of the sequence is not there; -1: find out.  ready: its query rows are in LDS, its first codes on their way (x).  more: piece n of the same sequence comes next, and is made ready.
 template <int HD, int NW>
-__device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, const KvPiece& p, bool holes, bool ready, const KvPiece& n, bool more,
+__device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, const KvPiece& p, int& holes, bool ready, const KvPiece& n, bool more,
                                            ManyShared<HD, NW>& sh, ManyAhead<HD, NW>& x, KvState<HD>& st) {
     constexpr int KS = HD / 16, DT = HD / 32, NT = 64 * NW, GB = 16 * HD, CHUNKS = 4 * HD, PER = ManyAhead<HD, NW>::PER;
     constexpr bool BOTH = CHUNKS >= NT;                                         // else half of the lanes have K, half V
@@ -412,11 +412,14 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
     // tiles [t0, t_plain) are seen whole by every column of the workgroup and have all their pages
     const int least = kv_end(a, q, (int)((uint32_t)(32 * NW * p.c) / (uint32_t)a.times));
     int t_plain = max(t0, min(t1, max(least, 0) / KV_TILE));
+    bool hole = false;
     if (!ready) {
         look_up(t0, page);
         look_up(t0 + 1, x.page1);
         ask_queries(p);
         fetch(p.h, t0, page);
+        if (holes < 0)
+            for (int i = anew(tid); i <= last >> a.c.page_shift; i += NT) hole |= (uint32_t)table[i] >= (uint32_t)a.c.n_pages;
         landed();
     }
     bf16x8 qf[KS];
@@ -425,12 +428,12 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
 #pragma unroll
         for (int k = 0; k < KS; ++k) qf[k] = *(const bf16x8*)(sh.rows[wave] + many_row<HD>(col_l, 4 * (k >> 1) + 2 * half + (k & 1)));
     }
+    if (holes < 0) holes = __syncthreads_or(hole);
+    else if (!holes) __syncthreads();                  // (either way:) the flags are cleared, and what the buffers held before has been read
     if (holes) {                                       // somewhere in the sequence: here?
-        bool hole = false;
+        hole = false;
         for (int i = (t0 * KV_TILE >> a.c.page_shift) + tid; i <= (t_plain * KV_TILE - 1) >> a.c.page_shift; i += NT) hole |= (uint32_t)table[i] >= (uint32_t)a.c.n_pages;
         if (__syncthreads_or(hole)) t_plain = t0;
-    } else {
-        __syncthreads();                               // the flags are cleared, and what the buffers held before has been read
     }
     auto convert = [&](int t, int buf) __attribute__((always_inline)) {
 #pragma unroll
@@ -619,9 +622,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
     if (f < f1) q = kv_find<COLS>(a, f, scan);
     while (f < f1) {
         const int64_t q_end = min(f1, q.first + q.head() * a.c.heads);
-        bool hole = false;
-        for (int i = threadIdx.x; i <= (q.len - 1) >> a.c.page_shift; i += 64 * NW) hole |= (uint32_t)a.c.table[(int64_t)q.b * a.c.table_stride + i] >= (uint32_t)a.c.n_pages;
-        const bool holes = __syncthreads_or(hole);
+        int holes = -1;
         ManyAhead<HD, NW> ahead;
         KvPiece n = kv_piece<COLS>(a, q, f, f1);
         for (bool ready = false; f < q_end;) {
