@@ -73,33 +73,31 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
     __shared__ __attribute__((aligned(16))) uint8_t stage[4][HD / 16 * STEP];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int item = blockIdx.x, B = a.c.n_seqs;
-    int b = -1;
+    // the last sequence that begins at or before the item, and its sizes: all that the search needs and finds comes with one access per 64 sequences
+    int b = -1, start = 0, end = 0, held = 0;
     for (int base = 0; base < B; base += 64) {
-        const int i = base + lane;
-        const bool before = i < B && (kv_clamped(a.cu[i], 0, a.n_tokens) >> 4) + 2 * i <= item;
-        b += __popcll(__ballot(before));
+        const int i = min(base + lane, B - 1);
+        const int c0 = a.cu[i], c1 = a.cu[i + 1], l = a.lens[i];
+        const int before = __popcll(__ballot(base + lane < B && (kv_clamped(c0, 0, a.n_tokens) >> 4) + 2 * i <= item));
+        if (before == 0) break;
+        b = base + before - 1;
+        start = __builtin_amdgcn_readlane(c0, before - 1);
+        end = __builtin_amdgcn_readlane(c1, before - 1);
+        held = __builtin_amdgcn_readlane(l, before - 1);
+        if (before < 64) break;
     }
     if (b < 0) return;
-    const int start = kv_clamped(a.cu[b], 0, a.n_tokens), n = kv_clamped(a.cu[b + 1], start, a.n_tokens) - start;
-    const int len = kv_clamped(a.lens[b], 0, a.c.capacity);
+    start = kv_clamped(start, 0, a.n_tokens);
+    const int n = kv_clamped(end, start, a.n_tokens) - start, len = kv_clamped(held, 0, a.c.capacity);
     const int nth = item - ((start >> 4) + 2 * b);
     const int64_t first = ((int64_t)(len >> 4) + nth) << 4;
     if (nth < 0 || first >= (int64_t)len + n || first >= a.c.capacity) return;
     const int p0 = (int)first, lo = max(len - p0, 0), hi = (int)min((int64_t)16, min((int64_t)len + n, (int64_t)a.c.capacity) - p0);      // new slots
-    if (lo >= hi || kv_group(a.c, b, 0, p0) < 0) return;
+    if (lo >= hi) return;
+    const int page = a.c.table[(int64_t)b * a.c.table_stride + (p0 >> a.c.page_shift)];               // (rows are asked for before it is there)
     const int pair = lane % PAIRS, s0 = lane / PAIRS * TPL;
     const int64_t row0 = start + (p0 - len);                                   // of slot 0; slots in [lo, hi) have a row
 
-    float cs[TPL], sn[TPL];
-    if constexpr (ROPE) {
-        const uint64_t turn = a.r.turn[pair];
-        const int axis = a.r.axis[pair];
-#pragma unroll
-        for (int t = 0; t < TPL; ++t) {
-            const int slot = kv_clamped(s0 + t, lo, hi - 1);
-            rope_sincos(turn, a.pos[(row0 + slot) * a.r.n_axes + axis], cs[t], sn[t]);
-        }
-    }
     Pair<T> k_raw[TPL], v_raw[TPL];
     const bool full = lo == 0 && hi == 16;
     auto load = [&](const void* from, int64_t stride, int64_t head, int h, Pair<T> (&raw)[TPL]) __attribute__((always_inline)) {
@@ -144,8 +142,19 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
         load(a.k, a.k_row, a.k_head, h, k_raw);
         load(a.v, a.v_row, a.v_head, h, v_raw);
     }
+    float cs[TPL], sn[TPL];
+    if constexpr (ROPE) {
+        const uint64_t turn = a.r.turn[pair];
+        const int axis = a.r.axis[pair];
+#pragma unroll
+        for (int t = 0; t < TPL; ++t) {
+            const int slot = kv_clamped(s0 + t, lo, hi - 1);
+            rope_sincos(turn, a.pos[(row0 + slot) * a.r.n_axes + axis], cs[t], sn[t]);
+        }
+    }
+    if ((uint32_t)page >= (uint32_t)a.c.n_pages) return;
     for (; h < a.c.heads; h += step) {
-        const int g = kv_group(a.c, b, h, p0);
+        const int g = kv_group_of(a.c, page, h, p0);
         uint8_t* const scale = a.c.scales + 2 * (int64_t)g;
         uint8_t* const kg = a.c.k + (int64_t)g * (16 * HD);
         uint8_t* const vg = a.c.v + (int64_t)g * (16 * HD);

@@ -20,11 +20,15 @@ struct KvView {
     int32_t capacity;                 // tokens that a row of the table has pages for
 };
 
-// Index of the group of position p (a multiple of KV_GROUP below capacity) of sequence b and head h; -1 where the table names no page.
+// Index of a page's group of head h with position p,
+__device__ __forceinline__ int kv_group_of(const KvView& c, int page, int h, int p) {
+    return ((page * c.heads + h) << (c.page_shift - 4)) + ((p & ((1 << c.page_shift) - 1)) >> 4);
+}
+// and that of position p (a multiple of KV_GROUP below capacity) of sequence b and head h; -1 where the table names no page.
 __device__ __forceinline__ int kv_group(const KvView& c, int b, int h, int p) {
     const int page = c.table[(int64_t)b * c.table_stride + (p >> c.page_shift)];
     if ((uint32_t)page >= (uint32_t)c.n_pages) return -1;
-    return ((page * c.heads + h) << (c.page_shift - 4)) + ((p & ((1 << c.page_shift) - 1)) >> 4);
+    return kv_group_of(c, page, h, p);
 }
 
 // Offsets of a ragged batch are the caller's device memory: whatever they hold, rows stay within [0, n_rows).
