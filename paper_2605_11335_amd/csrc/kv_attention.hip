@@ -660,7 +660,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_attend_many_kernel(AttendArgs a
             }
             if (cols > 0 && (p.whole || joined)) {
                 // rows of 2 head_dim bytes, 16 per lane: stored by dims of a lane, an instruction would touch 32 rows.  Past the caches, which have the keys and
-                // values that all workgroups share (13640 queries x 512 tokens x 24 heads: 115.8 us, 119.8 through them).
+                // values that all workgroups share (13640 queries x 512 tokens x 24 heads: 122 us, 129 through them).
                 const float inv = kv_inverse(l);
                 const int ln = anew(lane), col_l = ln & 31, half = ln >> 5;
                 char* const rows = (char*)&sh.k + wave * (64 * HD);            // where tiles were: k and v are as large as the outputs
@@ -829,23 +829,23 @@ constexpr int FEW_WGS = 512, MANY_WGS = 256;           // two workgroups on each
 // Whether column tiles are left whole, a workgroup to each, and nothing has to be joined.  `tiles`: of the longest sequence the table has room for, which
 // is all that the host knows.
 // Few columns: as long as all column tiles run at once and their keys, FEW_WAVES tiles at a time, take little longer than shares of them would, and
-// six such steps for the joining.  One query each, 8 key heads, whole / cut: 1 sequence of 1024 tokens 11.9 / 13.1 us, of 2048 16.4 / 12.9; 16 of 2048
-// 17.9 / 22.2, 64 of 2048 52.7 / 55.1; 256 of 512 74.8 / 61.8.
+// nine such steps for the joining.  One query each, 8 key heads, whole / cut: 1 sequence of 2048 tokens 16.1 / 17.0 us, of 2560 18.5 / 17.0; 8 of 2048
+// 17.3 / 22.2, of 3584 23.6 / 21.4; 32 of 4096 46.1 / 52.0; 256 of 512 63.4 / 50.5.
 bool few_whole(int64_t units, int64_t tiles) {
     const int64_t steps = (tiles + FEW_WAVES - 1) / FEW_WAVES;
-    return units <= FEW_WGS && steps <= steps * units / FEW_WGS + 6;
+    return units <= FEW_WGS && steps <= steps * units / FEW_WGS + 9;
 }
-// Many: 1.9 us per tile and 12 for the ends of a column tile, in whole rounds of workgroups, against equal shares and 25 us for leaving and joining their
-// pieces.  24 heads, whole / cut: 2560 queries x 2048 keys 74 / 98 us, 5461 x 512 73 / 77, 5461 x 2048 187 / 167, 10922 x 2048 313 / 293,
-// 21845 x 512 213 / 207, 43690 x 512 385 / 370.
+// Many: 1.55 us per tile and 9 for the ends of a column tile, in whole rounds of workgroups, against equal shares and 15 us for leaving and joining their
+// pieces.  24 heads, whole / cut: 2560 queries x 2048 keys 65 / 75 us, 3584 x 512 43.6 / 46.0, x 1024 67.7 / 62.2, 4608 x 512 43.4 / 50.7, 5461 x 512
+// 64 / 55, x 2048 178 / 140, 7168 x 512 64.5 / 66.0, 8448 x 512 85 / 74, 43690 x 512 360 / 333.
 bool many_whole(int64_t units, int64_t tiles) {
-    const double one = 12.0 + 1.9 * (double)tiles, rounds = (double)((units + MANY_WGS - 1) / MANY_WGS);
-    return rounds * one <= (double)units * one / MANY_WGS + 25.0;
+    const double one = 9.0 + 1.55 * (double)tiles, rounds = (double)((units + MANY_WGS - 1) / MANY_WGS);
+    return rounds * one <= (double)units * one / MANY_WGS + 15.0;
 }
 
 // Which kernel, by estimates of both (us; us per key tile of a column tile of 32 or 256 columns, all CUs at work, `fill` of the 256 taken).  32 / 8 heads,
-// few / many: 1 sequence of 8192 tokens, 64 queries 31 / 42; 8 of 8192, 12 queries each 55 / 56, 24 76 / 56, 64 171 / 87; 32 of 1024, 16 queries 29 / 31,
-// 24 43 / 32; 32 of 8192, 8 queries 98 / 147, 16 166 / 156, 64 633 / 269.
+// few / many: 1 sequence of 8192 tokens, 64 queries 29 / 39; 8 of 8192, 12 queries each 54 / 53, 24 76 / 54, 64 164 / 82; 32 of 1024, 16 queries 26 / 27,
+// 24 38 / 27; 32 of 8192, 8 queries 96 / 142, 16 157 / 145, 64 598 / 271.
 bool many_columns(double few_tiles, double many_tiles, double fill) {
     return 10.0 + 2.4e-3 * few_tiles > std::max(32.0, 14.0 + 1e-3 * (3.4 + 4.2 * fill) * many_tiles);
 }

@@ -66,7 +66,7 @@ __device__ __forceinline__ int64_t kv_lane64(int64_t x, int lane) {
 template <int COLS>
 __device__ __forceinline__ void kv_weigh(const AttendArgs& a, KvSeq& s) {
     s.ct = (s.n * a.times + COLS - 1) / COLS;
-    constexpr int ENDS = COLS == 32 ? 4 * KV_TILE : 6 * KV_TILE;           // 5 us of a workgroup alone, 12 us with all of them at their queries and outputs
+    constexpr int ENDS = COLS == 32 ? 4 * KV_TILE : 6 * KV_TILE;           // about 4 us, and 9 with all workgroups at their queries and outputs
     s.w0 = s.len + ENDS;
     s.dw = 0;
     if (a.whole) {
