@@ -545,13 +545,13 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
         ask_queries(n);
     }
     // tile t is in buffer (t - t0) & 1
-    auto plain = [&](int t, int buf) __attribute__((always_inline)) {
+    auto plain = [&](int t, int buf, bool fresh) __attribute__((always_inline)) {
         copies(t, buf);
         __builtin_amdgcn_sched_barrier(0);
         scores(buf);
         first_values(buf);
         __builtin_amdgcn_sched_barrier(0);
-        kv_softmax<HD>(st, s, a.c2, pf, t == t0);
+        kv_softmax<HD>(st, s, a.c2, pf, fresh);
         __builtin_amdgcn_sched_barrier(0);
         values(buf);
         __syncthreads();                               // tile t + 1 is in its buffer, that of t is free
@@ -592,10 +592,12 @@ __device__ __forceinline__ void many_sweep(const AttendArgs& a, const KvSeq& q, 
     };
     int t = t0;
     if (cols > 0) {
+        if (t < t_plain) plain(t++, 0, true);
         for (; t + 2 <= t_plain; t += 2) {             // (buffers known at compile time: addresses are a lane's offset and a constant)
-            plain(t, 0);
-            plain(t + 1, 1);
+            plain(t, 1, false);
+            plain(t + 1, 0, false);
         }
+        if (t < t_plain) plain(t++, 1, false);
     }
     for (; t < t1; ++t) any(t, (t - t0) & 1);
     if (more) {
